@@ -155,6 +155,17 @@ int unipool_route_bwd(const unipool_shape* shape, const void* x, const void* w_r
                       void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * unipool_route_bwd with the gradients of further losses: d_logits [T, E] float is added to dz (before dz is rounded in
+ * bfloat16 mode) and d_sigma_in [1] float to d_sigma, e.g. those of unipool_seq_balance_loss.  Either may be NULL; with
+ * both NULL the results are those of unipool_route_bwd.
+ */
+int unipool_route_bwd_add(const unipool_shape* shape, const void* x, const void* w_router,
+                          const float* logits, const int32_t* topk_idx, const float* dgate,
+                          const float* aux_coef, const float* d_logits, const float* d_sigma_in,
+                          float* d_w_router, float* d_sigma, void* dx, int dx_accumulate,
+                          void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Dispatch: expert-contiguous copy of the tokens (the grouping a grouped GEMM needs;
  * Table 7 only says that grouped GEMM is used, the row order is this library's).
  *   expert_offsets = exclusive prefix sum of counts, expert_offsets[E] = S;
@@ -295,6 +306,73 @@ int unipool_combine_bwd(const unipool_shape* shape, const void* dout, const void
 int unipool_pool_aux_loss(const unipool_shape* shape, const int32_t* counts, const float* psum,
                           const float* fbar_in, int32_t* pool_counts, float* fbar_out,
                           float* loss, float* aux_coef, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Balance loss of ONE layer over the sequences of a batch, with its gradient (Eq. 3 taken over every sequence by itself
+ * instead of over all tokens of the layer).  Sequence b is the tokens [seq_offsets[b], seq_offsets[b+1]), T_b of them:
+ *   counts[b, i] = number of (t, j) of the sequence with topk_idx[t, j] == i
+ *   f_{b,i} = E counts[b, i] / (k T_b);   P_{b,i} = (1/T_b) sum_t s_{t,i}   (s: the router's score, as for psum of unipool_route)
+ *   loss = alpha_seq (1/B') sum_b sum_i f_{b,i} P_{b,i},   B' = number of sequences that hold tokens
+ *   d_logits[t, i] = d loss / d logits[t, i],  d_sigma = d loss / d sigma   (f is constant for differentiation; softmax: d_sigma = 0)
+ * Sequences may be empty: their counts are zero and they add nothing.  Tokens outside all sequences (padding in front of the first or
+ * behind the last) are not read into any sum, and their rows of d_logits are zero.  seq_offsets must not decrease; what lies
+ * outside [0, T] is cut off.
+ * in : seq_offsets [n_seq + 1] int32 (device), 1 <= n_seq <= 2^20;  logits [T, E] float and topk_idx [T, k] from unipool_route.
+ * out: counts [n_seq, E] int32;  loss [1] float;  d_logits [T, E] float or NULL;  d_sigma [1] float or NULL.
+ */
+int unipool_seq_balance_loss(const unipool_shape* shape, int n_seq, const int32_t* seq_offsets, float alpha_seq,
+                             const float* logits, const int32_t* topk_idx, int32_t* counts, float* loss,
+                             float* d_logits, float* d_sigma, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Root-mean-square norm of the rows in front of a layer, with the addition of the residual.
+ *   h = x + residual (h = x if residual is NULL);   y = h / sqrt(mean(h^2) + norm_eps) * weight
+ * All of it in float; y is made from the unrounded h.  y may leave as act, in 8 bits (MX8, below), or both: the router reads the
+ * one, unipool_expert_ffn_fwd_mx8 the other.
+ * in : x [T, d] act;  residual [T, d] act or NULL;  weight [d] act;  norm_eps >= 0;  d <= 16384.
+ * out: h [T, d] act or NULL (may be x or residual itself);  y [T, d] act or NULL;  y_q [T, d] and y_scale in MX8, or both NULL
+ *      (needs d to be a multiple of 32).  One of y and y_q must be given.
+ */
+int unipool_rmsnorm(const unipool_shape* shape, const void* x, const void* residual, const void* weight, float norm_eps,
+                    void* h, void* y, void* y_q, void* y_scale, void* stream);
+
+/*
+ * Backward of unipool_rmsnorm, from the stored h.  With s = 1 / sqrt(mean(h^2) + norm_eps) and g = weight dy:
+ *   dx = s g - h s^3 mean(g h) + dh;   d_weight = sum_t dy h s
+ * dx is the gradient of x and of the residual alike.
+ * in : h [T, d] act;  weight [d] act;  dy [T, d] act;  dh [T, d] act or NULL (what else reaches h: the residual path).
+ * out: dx [T, d] act (may be dy or dh itself);  d_weight [d] float (overwritten).
+ */
+int unipool_rmsnorm_bwd(const unipool_shape* shape, const void* h, const void* weight, const void* dy, const void* dh,
+                        float norm_eps, void* dx, float* d_weight, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * MX8: 8-bit floats with block scales.  Values are e4m3 bytes, row-major; every 32 neighbours of a row share a scale 2^e, held
+ * as the byte e + 127.  e is the smallest integer >= -127 for which the largest magnitude of the block is at most 448 * 2^e;
+ * values are v / 2^e rounded to e4m3, to nearest even.  A block with a NaN or an infinity has scale byte 255 and NaN values.
+ * The scales of a matrix [rows, cols] lie as [ceil(cols / 128)][rows][4], one byte per block; bytes past cols are 127.
+ *
+ * unipool_quantize_mx8 lays a matrix out so, e.g. once the weights of the pool: w_gate_up as 2 d_ff E rows of d_model,
+ * w_down as d_model E rows of d_ff.
+ * in : src [rows, cols] float (dtype UNIPOOL_F32) or bfloat16 (UNIPOOL_BF16);  cols a multiple of 32;
+ *      ceil(rows / 64) * ceil(cols / 128) < 2^31.
+ * out: q [rows, cols] bytes;  scale [ceil(cols / 128), rows, 4] bytes.
+ */
+int unipool_quantize_mx8(int dtype, long long rows, int cols, const void* src, void* q, void* scale, void* stream);
+
+/*
+ * Pool experts on their row groups with rows and weights in MX8 (bfloat16 mode; forward only, for serving):
+ *   A = X_e W_gate,e^T;  B = X_e W_up,e^T;  H = silu(A) * B, rounded to MX8;  Y = H W_down,e^T, rounded to bfloat16.
+ * Products of 8-bit values are added in float on the matrix cores.
+ * in : x_q, x_scale: the tokens [T, d] in MX8 when slot_of_row is given (row r of the group order is token slot_of_row[r] / k), or the
+ *      rows [S, d] in group order when it is NULL;  expert_offsets [E+1];  w_gate_up_q [E, 2 d_ff, d], w_down_q [E, d, d_ff] with
+ *      their scales.  The values and y_perm must be aligned to 16 bytes, the scales to 4.
+ * out: h_q [S, d_ff], h_scale (H in MX8);  y_perm [S, d] bfloat16.
+ */
+int unipool_expert_ffn_fwd_mx8(const unipool_shape* shape, const void* x_q, const void* x_scale, const int32_t* slot_of_row,
+                               const int32_t* expert_offsets, const void* w_gate_up_q, const void* w_gate_up_scale,
+                               const void* w_down_q, const void* w_down_scale, void* h_q, void* h_scale, void* y_perm,
+                               void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Monte-Carlo estimate of the NormRouter calibration constant c (App. H (NormRouter Monte Carlo initialization), Alg. 1) from draws

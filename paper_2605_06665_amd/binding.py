@@ -32,7 +32,8 @@ ENTRY_POINTS = ("unipool_workspace_bytes", "unipool_last_error", "unipool_versio
                 "unipool_route_bwd", "unipool_permute", "unipool_permute_static", "unipool_expert_ffn_fwd", "unipool_expert_ffn_fwd_gather",
                 "unipool_expert_ffn_recompute", "unipool_expert_ffn_bwd", "unipool_expert_wgrad", "unipool_combine",
                 "unipool_combine_bwd", "unipool_pool_aux_loss", "unipool_estimate_c",
-                "unipool_distinct_experts")
+                "unipool_distinct_experts", "unipool_route_bwd_add", "unipool_seq_balance_loss", "unipool_rmsnorm", "unipool_rmsnorm_bwd",
+                "unipool_quantize_mx8", "unipool_expert_ffn_fwd_mx8")
 
 
 def lib_path() -> str:
@@ -48,7 +49,7 @@ def load_library():
             raise UniPoolError(
                 "%s is missing: build it first (python -c 'import __graft_entry__ as g; g.build()')" % path)
         lib = ctypes.CDLL(path)
-        P, I, Z = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+        P, I, Z, F = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_float
         SP = ctypes.POINTER(Shape)
         lib.unipool_workspace_bytes.restype = Z
         lib.unipool_workspace_bytes.argtypes = [SP]
@@ -75,6 +76,12 @@ def load_library():
             "unipool_pool_aux_loss": [SP] + [P] * 7 + [P, Z, P],
             "unipool_estimate_c": [I, I, P, I, P, P, P, Z, P],
             "unipool_distinct_experts": [SP, I, P, P, P, P, Z, P],
+            "unipool_route_bwd_add": [SP] + [P] * 11 + [I, P, Z, P],
+            "unipool_seq_balance_loss": [SP, I, P, F] + [P] * 6 + [P, Z, P],
+            "unipool_rmsnorm": [SP] + [P] * 3 + [F] + [P] * 4 + [P],
+            "unipool_rmsnorm_bwd": [SP] + [P] * 4 + [F, P, P] + [P, Z, P],
+            "unipool_quantize_mx8": [I, ctypes.c_longlong, I] + [P] * 4,
+            "unipool_expert_ffn_fwd_mx8": [SP] + [P] * 11 + [P, Z, P],
         }
         for name, argtypes in sigs.items():
             fn = getattr(lib, name)
@@ -267,3 +274,55 @@ def distinct_experts(shape, n_layers, topk_idx_tab, distinct, mean_distinct, ws,
     _check(load_library().unipool_distinct_experts(ctypes.byref(shape), int(n_layers), _ptr(topk_idx_tab),
                                                    _ptr(distinct), _ptr(mean_distinct), p, n, _stream(stream)),
            "unipool_distinct_experts")
+
+
+def route_bwd_add(shape, x, w_router, logits, topk_idx, dgate, aux_coef, d_logits, d_sigma_in, d_w_router, d_sigma, dx,
+                  dx_accumulate, ws, stream=None):
+    """route_bwd with d_logits [T, E] and d_sigma_in [1] (float32, either may be None) added to the gradients of logits and sigma."""
+    p, n = _ws(ws)
+    _check(load_library().unipool_route_bwd_add(ctypes.byref(shape), _ptr(x), _ptr(w_router), _ptr(logits), _ptr(topk_idx),
+                                                _ptr(dgate), _ptr(aux_coef), _ptr(d_logits), _ptr(d_sigma_in),
+                                                _ptr(d_w_router), _ptr(d_sigma), _ptr(dx), int(bool(dx_accumulate)), p, n,
+                                                _stream(stream)), "unipool_route_bwd_add")
+
+
+def seq_balance_loss(shape, n_seq, seq_offsets, alpha_seq, logits, topk_idx, counts, loss, d_logits, d_sigma, ws, stream=None):
+    """Balance loss of a layer over the sequences [seq_offsets[b], seq_offsets[b + 1]) and its gradient; d_logits, d_sigma may be None."""
+    p, n = _ws(ws)
+    _check(load_library().unipool_seq_balance_loss(ctypes.byref(shape), int(n_seq), _ptr(seq_offsets), float(alpha_seq), _ptr(logits),
+                                                   _ptr(topk_idx), _ptr(counts), _ptr(loss), _ptr(d_logits), _ptr(d_sigma), p, n,
+                                                   _stream(stream)), "unipool_seq_balance_loss")
+
+
+def rmsnorm(shape, x, residual, weight, norm_eps, h, y, y_q, y_scale, stream=None):
+    """residual, h, y may be None, and y_q with y_scale; y or y_q must be given."""
+    _check(load_library().unipool_rmsnorm(ctypes.byref(shape), _ptr(x), _ptr(residual), _ptr(weight), float(norm_eps), _ptr(h),
+                                          _ptr(y), _ptr(y_q), _ptr(y_scale), _stream(stream)), "unipool_rmsnorm")
+
+
+def rmsnorm_bwd(shape, h, weight, dy, dh, norm_eps, dx, d_weight, ws, stream=None):
+    """dh may be None; dx may be dy or dh."""
+    p, n = _ws(ws)
+    _check(load_library().unipool_rmsnorm_bwd(ctypes.byref(shape), _ptr(h), _ptr(weight), _ptr(dy), _ptr(dh), float(norm_eps),
+                                              _ptr(dx), _ptr(d_weight), p, n, _stream(stream)), "unipool_rmsnorm_bwd")
+
+
+def mx8_scale_shape(rows, cols):
+    """Shape of the uint8 tensor with the scales of a matrix in MX8."""
+    return (-(-cols // 128), rows, 4)
+
+
+def quantize_mx8(dtype, rows, cols, src, q, scale, stream=None):
+    """src [rows, cols] (dtype F32 or BF16) to e4m3 bytes q [rows, cols] and scales of mx8_scale_shape(rows, cols), both uint8."""
+    _check(load_library().unipool_quantize_mx8(int(dtype), int(rows), int(cols), _ptr(src), _ptr(q), _ptr(scale), _stream(stream)),
+           "unipool_quantize_mx8")
+
+
+def expert_ffn_fwd_mx8(shape, x_q, x_scale, slot_of_row, expert_offsets, w_gate_up_q, w_gate_up_scale, w_down_q, w_down_scale,
+                       h_q, h_scale, y_perm, ws, stream=None):
+    """slot_of_row None: x_q holds the rows in group order instead of the tokens."""
+    p, n = _ws(ws)
+    _check(load_library().unipool_expert_ffn_fwd_mx8(ctypes.byref(shape), _ptr(x_q), _ptr(x_scale), _ptr(slot_of_row),
+                                                     _ptr(expert_offsets), _ptr(w_gate_up_q), _ptr(w_gate_up_scale),
+                                                     _ptr(w_down_q), _ptr(w_down_scale), _ptr(h_q), _ptr(h_scale),
+                                                     _ptr(y_perm), p, n, _stream(stream)), "unipool_expert_ffn_fwd_mx8")

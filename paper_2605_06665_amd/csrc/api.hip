@@ -76,7 +76,7 @@ WsLayout ws_layout(const unipool_shape& s) {
     w.cnt_part = o;    o += align_up(rblocks * E * sizeof(int32_t));
     w.dz = o;          o += align_up(std::max(T * E * 4, T * ez * act));   // logits (float) or dz
     w.ptr_tab = o;     o += 256;
-    w.wpart = o;       o += align_up((size_t)kRouteBwdSplit * ez * d * sizeof(float));
+    w.wpart = o;       o += align_up(std::max((size_t)kRouteBwdSplit * ez, (size_t)kNormParts) * d * sizeof(float));
     w.total = o;
     return w;
 }
@@ -131,11 +131,34 @@ int32_t* extra_table(const unipool_shape& s, const WsLayout& w, void* ws) {
         int rc_ = unipool::validate_shape(shape, __func__);                         \
         if (rc_) return rc_;                                                  \
     }
+#define NORM_CHECKS()                                                                                                      \
+    if (shape->d_model > kNormMaxD)                                                                                       \
+        return set_error(UNIPOOL_EINVAL, "%s: d_model=%d above %d", __func__, shape->d_model, kNormMaxD);                  \
+    if (!(norm_eps >= 0.f)) return set_error(UNIPOOL_EINVAL, "%s: norm_eps must be non-negative", __func__)
 #define NEED_WS()                                                             \
     {                                                                         \
         int rc_ = unipool::need_ws(shape, ws, ws_bytes, __func__);            \
         if (rc_) return rc_;                                                  \
     }
+
+int route_bwd(const unipool_shape& s, const char* fn, const void* x, const void* w_router, const float* logits,
+              const int32_t* topk_idx, const float* dgate, const float* aux_coef, const float* d_logits, const float* d_sigma_in,
+              float* d_w_router, float* d_sigma, void* dx, int dx_accumulate, char* base, hipStream_t st) {
+    const WsLayout w = ws_layout(s);
+    void* dz = base + w.dz;
+    float* dsigma_part = (float*)(base + w.psum_part);
+    const bool mfma = mfma_route_bwd_supported(s, x, w_router, dx);
+    hipError_t e = launch_route_bwd_dz(s, logits, topk_idx, dgate, aux_coef, d_logits, d_sigma_in, dz, dsigma_part, st);
+    if (e == hipSuccess) {
+        if (mfma)
+            e = mfma_route_bwd_mm(s, x, w_router, dz, d_w_router, dx, dx_accumulate, dsigma_part, d_sigma, (float*)(base + w.wpart), st);
+        else
+            e = f32_route_bwd_mm(s, x, w_router, dz, d_w_router, dx, dx_accumulate, dsigma_part, d_sigma, (float*)(base + w.wpart), st);
+    }
+    return check_hip(e, fn);
+}
+
+bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
 }  // namespace
 }  // namespace unipool
@@ -213,21 +236,21 @@ int unipool_route_bwd(const unipool_shape* shape, const void* x, const void* w_r
     REQUIRE_PTR(x); REQUIRE_PTR(w_router); REQUIRE_PTR(logits); REQUIRE_PTR(topk_idx);
     REQUIRE_PTR(dgate); REQUIRE_PTR(d_w_router); REQUIRE_PTR(d_sigma); REQUIRE_PTR(dx);
     NEED_WS();
-    const WsLayout w = ws_layout(*shape);
-    char* base = (char*)ws;
-    hipStream_t st = (hipStream_t)stream;
-    void* dz = base + w.dz;
-    float* dsigma_part = (float*)(base + w.psum_part);
-    const bool mfma = mfma_route_bwd_supported(*shape, x, w_router, dx);
-    hipError_t e = launch_route_bwd_dz(*shape, logits, topk_idx, dgate, aux_coef, dz, dsigma_part, st);
-    if (e != hipSuccess) return check_hip(e, "unipool_route_bwd: dz");
-    if (mfma)
-        e = mfma_route_bwd_mm(*shape, x, w_router, dz, d_w_router, dx, dx_accumulate, dsigma_part, d_sigma,
-                              (float*)(base + w.wpart), st);
-    else
-        e = f32_route_bwd_mm(*shape, x, w_router, dz, d_w_router, dx, dx_accumulate, dsigma_part, d_sigma,
-                             (float*)(base + w.wpart), st);
-    return check_hip(e, "unipool_route_bwd: contractions");
+    return route_bwd(*shape, __func__, x, w_router, logits, topk_idx, dgate, aux_coef, nullptr, nullptr, d_w_router,
+                     d_sigma, dx, dx_accumulate, (char*)ws, (hipStream_t)stream);
+}
+
+int unipool_route_bwd_add(const unipool_shape* shape, const void* x, const void* w_router,
+                          const float* logits, const int32_t* topk_idx, const float* dgate,
+                          const float* aux_coef, const float* d_logits, const float* d_sigma_in,
+                          float* d_w_router, float* d_sigma, void* dx,
+                          int dx_accumulate, void* ws, size_t ws_bytes, void* stream) {
+    PROLOGUE();
+    REQUIRE_PTR(x); REQUIRE_PTR(w_router); REQUIRE_PTR(logits); REQUIRE_PTR(topk_idx);
+    REQUIRE_PTR(dgate); REQUIRE_PTR(d_w_router); REQUIRE_PTR(d_sigma); REQUIRE_PTR(dx);
+    NEED_WS();
+    return route_bwd(*shape, __func__, x, w_router, logits, topk_idx, dgate, aux_coef, d_logits, d_sigma_in, d_w_router,
+                     d_sigma, dx, dx_accumulate, (char*)ws, (hipStream_t)stream);
 }
 
 int unipool_permute(const unipool_shape* shape, const void* x, const int32_t* topk_idx,
@@ -441,6 +464,77 @@ int unipool_distinct_experts(const unipool_shape* shape, int n_layers, const voi
                                              distinct, (int32_t*)((char*)ws + w.psum_part), mean_distinct,
                                              (hipStream_t)stream),
                      "unipool_distinct_experts");
+}
+
+int unipool_rmsnorm(const unipool_shape* shape, const void* x, const void* residual, const void* weight, float norm_eps,
+                    void* h, void* y, void* y_q, void* y_scale, void* stream) {
+    PROLOGUE();
+    NORM_CHECKS();
+    REQUIRE_PTR(x); REQUIRE_PTR(weight);
+    if (!y && !y_q) return set_error(UNIPOOL_EINVAL, "%s: neither y nor y_q is given", __func__);
+    if ((y_q == nullptr) != (y_scale == nullptr))
+        return set_error(UNIPOOL_EINVAL, "%s: y_q and y_scale must both be given or both be NULL", __func__);
+    if (y_q && shape->d_model % 32 != 0)
+        return set_error(UNIPOOL_EINVAL, "%s: 8-bit output needs d_model to be a multiple of 32 (d=%d)", __func__, shape->d_model);
+    return check_hip(launch_rmsnorm(*shape, x, residual, weight, norm_eps, h, y, y_q, y_scale, (hipStream_t)stream), __func__);
+}
+
+int unipool_rmsnorm_bwd(const unipool_shape* shape, const void* h, const void* weight, const void* dy, const void* dh,
+                        float norm_eps, void* dx, float* d_weight, void* ws, size_t ws_bytes, void* stream) {
+    PROLOGUE();
+    NORM_CHECKS();
+    REQUIRE_PTR(h); REQUIRE_PTR(weight); REQUIRE_PTR(dy); REQUIRE_PTR(dx); REQUIRE_PTR(d_weight);
+    NEED_WS();
+    const WsLayout w = ws_layout(*shape);
+    return check_hip(launch_rmsnorm_bwd(*shape, h, weight, dy, dh, norm_eps, dx, d_weight, (float*)((char*)ws + w.wpart),
+                                        (hipStream_t)stream), __func__);
+}
+
+int unipool_seq_balance_loss(const unipool_shape* shape, int n_seq, const int32_t* seq_offsets, float alpha_seq,
+                             const float* logits, const int32_t* topk_idx, int32_t* counts, float* loss, float* d_logits,
+                             float* d_sigma, void* ws, size_t ws_bytes, void* stream) {
+    PROLOGUE();
+    if (n_seq < 1 || n_seq > (1 << 20))
+        return set_error(UNIPOOL_EINVAL, "%s: n_seq=%d outside [1, 2^20]", __func__, n_seq);
+    REQUIRE_PTR(seq_offsets); REQUIRE_PTR(logits); REQUIRE_PTR(topk_idx); REQUIRE_PTR(counts); REQUIRE_PTR(loss);
+    NEED_WS();
+    const WsLayout w = ws_layout(*shape);
+    char* base = (char*)ws;
+    return check_hip(launch_seq_balance_loss(*shape, n_seq, seq_offsets, alpha_seq, logits, topk_idx, counts, loss, d_logits, d_sigma,
+                                             (int32_t*)(base + w.cnt_part), (float*)(base + w.psum_part),
+                                             (int32_t*)(base + w.ptr_tab), (hipStream_t)stream), __func__);
+}
+
+int unipool_quantize_mx8(int dtype, long long rows, int cols, const void* src, void* q, void* scale, void* stream) {
+    if (dtype != UNIPOOL_F32 && dtype != UNIPOOL_BF16)
+        return set_error(UNIPOOL_EINVAL, "%s: dtype %d is neither UNIPOOL_F32 nor UNIPOOL_BF16", __func__, dtype);
+    if (rows < 1 || cols < 1 || cols % 32 != 0)
+        return set_error(UNIPOOL_EINVAL, "%s: rows must be positive and cols a positive multiple of 32 (rows=%lld cols=%d)", __func__,
+                         rows, cols);
+    if (rows > (1LL << 40) || (rows + 63) / 64 * cdiv(cols, 128) >= (1LL << 31))
+        return set_error(UNIPOOL_EINVAL, "%s: matrix of %lld x %d is too large for one call", __func__, rows, cols);
+    REQUIRE_PTR(src); REQUIRE_PTR(q); REQUIRE_PTR(scale);
+    return check_hip(launch_quantize_mx8(dtype, src, rows, cols, q, scale, (hipStream_t)stream), __func__);
+}
+
+int unipool_expert_ffn_fwd_mx8(const unipool_shape* shape, const void* x_q, const void* x_scale, const int32_t* slot_of_row,
+                               const int32_t* expert_offsets, const void* w_gate_up_q, const void* w_gate_up_scale,
+                               const void* w_down_q, const void* w_down_scale, void* h_q, void* h_scale, void* y_perm,
+                               void* ws, size_t ws_bytes, void* stream) {
+    PROLOGUE();
+    if (shape->dtype != UNIPOOL_BF16)
+        return set_error(UNIPOOL_EINVAL, "%s: experts in 8 bits exist in bfloat16 mode only", __func__);
+    REQUIRE_PTR(x_q); REQUIRE_PTR(x_scale); REQUIRE_PTR(expert_offsets); REQUIRE_PTR(w_gate_up_q); REQUIRE_PTR(w_gate_up_scale);
+    REQUIRE_PTR(w_down_q); REQUIRE_PTR(w_down_scale); REQUIRE_PTR(h_q); REQUIRE_PTR(h_scale); REQUIRE_PTR(y_perm);
+    if (!aligned(x_q, 16) || !aligned(w_gate_up_q, 16) || !aligned(w_down_q, 16) || !aligned(h_q, 16) || !aligned(y_perm, 16))
+        return set_error(UNIPOOL_EINVAL, "%s: x_q, w_gate_up_q, w_down_q, h_q and y_perm must be aligned to 16 bytes", __func__);
+    if (!aligned(x_scale, 4) || !aligned(w_gate_up_scale, 4) || !aligned(w_down_scale, 4) || !aligned(h_scale, 4))
+        return set_error(UNIPOOL_EINVAL, "%s: scales must be aligned to 4 bytes", __func__);
+    NEED_WS();
+    const WsLayout w = ws_layout(*shape);
+    return check_hip(mx8_ffn_fwd(*shape, x_q, x_scale, slot_of_row, expert_offsets, w_gate_up_q, w_gate_up_scale, w_down_q,
+                                 w_down_scale, h_q, h_scale, y_perm, (int32_t*)((char*)ws + w.tile_meta), (hipStream_t)stream),
+                     __func__);
 }
 
 }  // extern "C"

@@ -104,15 +104,17 @@ struct WsLayout {
     size_t cnt_part;       // int32 [ceil(T/64)][E] partial counts
     size_t dz;             // act   [T][dz_stride]  router backward logits gradient; float [T][E] logits
     size_t ptr_tab;        // 5 device pointers for the single-layer weight gradient
-    size_t wpart;          // float [split][dz_stride][d]  router weight gradient partials
+    size_t wpart;          // float [split][dz_stride][d]  router weight gradient partials; [kNormParts][d] of the norm's
     size_t total;
 };
 WsLayout ws_layout(const unipool_shape& s);
 
 constexpr int kRouterTokensPerBlock = 64;   // tokens per block in the per-token router kernels
 constexpr int kRouteBwdSplit = 64;          // max row chunks of the router weight-gradient reduction
+constexpr int kNormMaxD = 16384;            // longest row of the norm
+constexpr int kNormParts = 512;             // max partial sums of the norm's weight gradient
 
-inline int cdiv(int a, int b) { return (a + b - 1) / b; }
+constexpr int cdiv(int a, int b) { return (a + b - 1) / b; }
 
 // Row length of dz: the bfloat16 products read it in chunks of eight values, so its rows are filled up with zeros.
 inline int dz_stride(const unipool_shape& s) { return s.dtype == UNIPOOL_BF16 ? cdiv(s.E, 8) * 8 : s.E; }

@@ -15,10 +15,10 @@ hipError_t launch_route_finalize(const unipool_shape& s, const int32_t* cnt_part
                                  int32_t* counts, float* psum, hipStream_t st);
 // Per-token backward of the score: writes dz (act dtype) and partial sums of d_sigma, which the kernels of the contractions add
 // up.  dsigma_part: one float per block of dz_tokens_per_block tokens, so 1, 4 or 8 floats per 64 tokens, never more than the E
-// that the area of the partial score sums, where they lie, has for 64 tokens.
+// that the area of the partial score sums, where they lie, has for 64 tokens.  d_logits, d_sigma_in: added to dz and d_sigma, or null.
 inline int dz_tokens_per_block(const unipool_shape& s) { return s.E < 4 ? kRouterTokensPerBlock : s.E <= 256 ? 16 : 8; }
 hipError_t launch_route_bwd_dz(const unipool_shape& s, const float* logits, const int32_t* topk_idx,
-                               const float* dgate, const float* aux_coef, void* dz,
+                               const float* dgate, const float* aux_coef, const float* d_logits, const float* d_sigma_in, void* dz,
                                float* dsigma_part, hipStream_t st);
 
 // ---- permute.hip ------------------------------------------------------------------
@@ -107,6 +107,27 @@ hipError_t few_ffn_gate_up(const unipool_shape& s, const void* x, const int32_t*
 hipError_t few_ffn_fwd(const unipool_shape& s, const void* x, const int32_t* offsets, const void* wgu, const void* wd,
                        void* a_out, void* b_out, void* h_out, void* y, hipStream_t st,
                        const int32_t* slot_of_row = nullptr);
+
+hipError_t mfma_build_tiles(const unipool_shape& s, const int32_t* offsets, int bm, int32_t* meta, hipStream_t st);
+
+// ---- norm.hip ---------------------------------------------------------------------
+hipError_t launch_rmsnorm(const unipool_shape& s, const void* x, const void* residual, const void* weight, float eps, void* h,
+                          void* y, void* y_q, void* y_scale, hipStream_t st);
+// part: [kNormParts][d] floats
+hipError_t launch_rmsnorm_bwd(const unipool_shape& s, const void* h, const void* weight, const void* dy, const void* dh, float eps,
+                              void* dx, float* d_weight, float* part, hipStream_t st);
+
+// ---- mx8.hip, ffn_mx8.hip: 8-bit values with block scales --------------------------
+hipError_t launch_quantize_mx8(int dtype, const void* src, long long rows, int cols, void* q, void* scale, hipStream_t st);
+hipError_t mx8_ffn_fwd(const unipool_shape& s, const void* x, const void* x_scale, const int32_t* slot_of_row, const int32_t* offsets,
+                       const void* wgu, const void* wgu_scale, const void* wd, const void* wd_scale, void* h, void* h_scale, void* y,
+                       int32_t* tile_meta, hipStream_t st);
+
+// ---- balance.hip -------------------------------------------------------------------
+// cnt_part and loss_part: the areas of the router's partial counts and score sums; state: two words
+hipError_t launch_seq_balance_loss(const unipool_shape& s, int n_seq, const int32_t* seq_offsets, float alpha, const float* logits,
+                                   const int32_t* topk_idx, int32_t* counts, float* loss, float* d_logits, float* d_sigma,
+                                   int32_t* cnt_part, float* loss_part, int32_t* state, hipStream_t st);
 
 // ---- small utilities (api.hip) ---------------------------------------------------------
 hipError_t launch_set_ptrs(void** table, const void* p0, const void* p1, const void* p2,

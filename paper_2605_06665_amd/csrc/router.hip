@@ -154,7 +154,8 @@ __global__ __launch_bounds__(256) void route_finalize_kernel(
 template <typename TA, int GS, int VPL>
 __global__ __launch_bounds__(256) void route_bwd_dz_kernel(
     const float* __restrict__ logits, const int32_t* __restrict__ topk_idx,
-    const float* __restrict__ dgate, const float* __restrict__ aux_coef, int T, int E, int k,
+    const float* __restrict__ dgate, const float* __restrict__ aux_coef, const float* __restrict__ d_logits,
+    const float* __restrict__ d_sigma_in, int T, int E, int k,
     float sigma, float c, float eps, int softmax, int tok_per_block, TA* __restrict__ dz, int ldz,
     float* __restrict__ dsigma_part) {
     constexpr int TPW = 64 / GS;
@@ -230,7 +231,11 @@ __global__ __launch_bounds__(256) void route_bwd_dz_kernel(
 #pragma unroll
                 for (int i = 0; i < VPL; i++) {
                     const int e = sl + GS * i;
-                    if (e < ldz) dz[(size_t)t * ldz + e] = from_f32<TA>(e < E ? pr[i] * (ds[i] - dotp) : 0.f);
+                    if (e < ldz) {
+                        float v = e < E ? pr[i] * (ds[i] - dotp) : 0.f;
+                        if (d_logits != nullptr && e < E) v += d_logits[(size_t)t * E + e];
+                        dz[(size_t)t * ldz + e] = from_f32<TA>(v);
+                    }
                 }
             }
             continue;
@@ -253,7 +258,8 @@ __global__ __launch_bounds__(256) void route_bwd_dz_kernel(
             for (int i = 0; i < VPL; i++) {
                 const int e = sl + GS * i;
                 if (e < ldz) {
-                    const float v = (n > 0.f && e < E) ? dzh[i] * inv - z[i] * back : 0.f;
+                    float v = (n > 0.f && e < E) ? dzh[i] * inv - z[i] * back : 0.f;
+                    if (d_logits != nullptr && e < E) v += d_logits[(size_t)t * E + e];
                     dz[(size_t)t * ldz + e] = from_f32<TA>(v);
                 }
             }
@@ -262,8 +268,11 @@ __global__ __launch_bounds__(256) void route_bwd_dz_kernel(
     dsig = wave_sum(dsig);
     if (lane == 0) lds_ds[wave] = dsig;
     __syncthreads();
-    if (threadIdx.x == 0)
-        dsigma_part[blockIdx.x] = ((lds_ds[0] + lds_ds[1]) + lds_ds[2]) + lds_ds[3];
+    if (threadIdx.x == 0) {
+        float v = ((lds_ds[0] + lds_ds[1]) + lds_ds[2]) + lds_ds[3];
+        if (d_sigma_in != nullptr && blockIdx.x == 0) v += d_sigma_in[0];
+        dsigma_part[blockIdx.x] = v;
+    }
 }
 
 }  // namespace
@@ -330,11 +339,11 @@ hipError_t launch_route_finalize(const unipool_shape& s, const int32_t* cnt_part
 }
 
 hipError_t launch_route_bwd_dz(const unipool_shape& s, const float* logits, const int32_t* topk_idx,
-                               const float* dgate, const float* aux_coef, void* dz,
+                               const float* dgate, const float* aux_coef, const float* d_logits, const float* d_sigma_in, void* dz,
                                float* dsigma_part, hipStream_t st) {
     const int tokens = dz_tokens_per_block(s), nblocks = cdiv(s.T, tokens);
 #define UNIPOOL_DZ(TA, GS, VPL)                                                                        \
-    route_bwd_dz_kernel<TA, GS, VPL><<<nblocks, 256, 0, st>>>(logits, topk_idx, dgate, aux_coef, s.T, s.E, \
+    route_bwd_dz_kernel<TA, GS, VPL><<<nblocks, 256, 0, st>>>(logits, topk_idx, dgate, aux_coef, d_logits, d_sigma_in, s.T, s.E, \
                                                               s.k, s.sigma, s.c, s.eps, s.router, tokens, (TA*)dz, dz_stride(s), dsigma_part)
     if (s.dtype == UNIPOOL_BF16) {
         if (s.E <= 128) UNIPOOL_DZ(bf16, 16, 8);
