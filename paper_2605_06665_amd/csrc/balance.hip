@@ -7,7 +7,8 @@
 // <coef, s_t> over the tokens.  coef follows from the picks alone, so the picks are counted first and ONE pass over the logits
 // then gives loss and gradient.  The score is linear in sigma: d loss / d sigma = loss / sigma (softmax: 0).
 //
-// Bound by memory: 4 bytes in and 4 out per logit, in the lane layout of the router's backward pass.
+// Bound by memory and by what a token costs in instructions and latency: 4 bytes in and 4 out per logit.  16384 tokens of 512
+// experts, k = 8, 37 sequences, softmax: counts 4.9 us, loss and gradient 19.2 us (67 MB, 3.5 TB/s).
 #include <algorithm>
 
 #include "route_select.h"
@@ -18,6 +19,11 @@ namespace unipool {
 namespace {
 
 constexpr int kTokensPerPart = 4096;      // tokens of a sequence that one workgroup counts
+constexpr int kCountThreads = 512;
+constexpr int kLossThreads = 1024;
+constexpr int kLossTokens = 64;           // tokens of a workgroup, a multiple of that from kLossBlocks workgroups on
+constexpr int kLossBlocks = 512;
+constexpr int kOneTokens = 256, kOneCounts = 8192;      // what a single workgroup does by itself
 
 struct SeqArgs {
     const int32_t* offsets;               // [n_seq + 1]
@@ -39,27 +45,31 @@ __device__ __forceinline__ void seq_range(const SeqArgs& a, int b, int& t0, int&
     t1 = min(max(a.offsets[b + 1], t0), a.T);
 }
 
-// Picks per expert of part blockIdx.y of sequence blockIdx.x.
-__global__ __launch_bounds__(256) void seq_count_kernel(const SeqArgs a) {
+// Picks per expert of part blockIdx.y of sequence blockIdx.x.  A thread requests eight picks at a time.
+__global__ __launch_bounds__(kCountThreads) void seq_count_kernel(const SeqArgs a) {
     __shared__ int hist[kMaxE];
-    __shared__ int used[4];
+    __shared__ int used[kCountThreads / 64];
     const int b = blockIdx.x, p = blockIdx.y;
-    for (int i = threadIdx.x; i < a.E; i += 256) hist[i] = 0;
+    for (int i = threadIdx.x; i < a.E; i += kCountThreads) hist[i] = 0;
     int t0, t1;
     seq_range(a, b, t0, t1);
     const int per = (int)(((long long)(t1 - t0) + a.parts - 1) / a.parts);
     const long long s0 = (long long)min(t0 + (long long)p * per, (long long)t1) * a.k, s1 = (long long)min(t0 + (long long)(p + 1) * per, (long long)t1) * a.k;
     __syncthreads();
-    for (long long s = s0 + threadIdx.x; s < s1; s += 256) {
-        const int e = a.topk_idx[s];
-        if (e >= 0 && e < a.E) atomicAdd(&hist[e], 1);
+    for (long long s = s0 + threadIdx.x; s < s1; s += 8 * kCountThreads) {
+        int e[8];
+#pragma unroll
+        for (int u = 0; u < 8; u++) e[u] = s + u * kCountThreads < s1 ? a.topk_idx[s + u * kCountThreads] : -1;
+#pragma unroll
+        for (int u = 0; u < 8; u++)
+            if (e[u] >= 0 && e[u] < a.E) atomicAdd(&hist[e[u]], 1);
     }
     __syncthreads();
     int32_t* out = (a.parts > 1 ? a.part + (size_t)p * a.n_seq * a.E : a.counts) + (size_t)b * a.E;
-    for (int i = threadIdx.x; i < a.E; i += 256) out[i] = hist[i];
+    for (int i = threadIdx.x; i < a.E; i += kCountThreads) out[i] = hist[i];
     if (b == 0 && p == 0) {
         int n = 0;
-        for (int i = threadIdx.x; i < a.n_seq; i += 256) {
+        for (int i = threadIdx.x; i < a.n_seq; i += kCountThreads) {
             int r0, r1;
             seq_range(a, i, r0, r1);
             n += r1 > r0;
@@ -68,7 +78,9 @@ __global__ __launch_bounds__(256) void seq_count_kernel(const SeqArgs a) {
         if ((threadIdx.x & 63) == 0) used[threadIdx.x >> 6] = n;
         __syncthreads();
         if (threadIdx.x == 0) {
-            a.state[0] = used[0] + used[1] + used[2] + used[3];
+            int all = 0;
+            for (int w = 0; w < kCountThreads / 64; w++) all += used[w];
+            a.state[0] = all;
             a.state[1] = 0;
         }
     }
@@ -82,40 +94,90 @@ __global__ __launch_bounds__(256) void seq_count_sum_kernel(const SeqArgs a) {
     a.counts[i] = v;
 }
 
-// GS lanes to a token, VPL logits to a lane: lane s holds logits s + GS i, or with V4 groups of four neighbours.
-template <int GS, int VPL, bool V4>
-__global__ __launch_bounds__(256) void seq_loss_kernel(const SeqArgs a) {
+// The sequence that holds token t, or else the next one that ends behind it: the first b with offsets[b + 1] > t, n_seq if there is
+// none.  By a wavefront, 64 places at a time.
+__device__ __forceinline__ int find_sequence(const SeqArgs& a, int t, int lane) {
+    int lo = 0, hi = a.n_seq;                         // the answer lies in [lo, hi]
+    while (lo < hi) {
+        const int step = (hi - lo + 63) >> 6;
+        const int at = lo + (lane + 1) * step - 1;    // last place of the lane's part
+        const unsigned long long over = __ballot(at >= hi || a.offsets[min(at, hi - 1) + 1] > t);
+        const int first = over ? __builtin_ctzll(over) : 64;
+        const int from = lo + first * step;
+        if (from >= hi) return hi;                     // every part that there is ends at or before t
+        hi = min(hi, from + step - 1);                 // (its last place is an answer)
+        lo = from;
+    }
+    return lo;
+}
+
+// GS lanes to a token, VPL logits to a lane: lane s holds logits s + GS i, or with V4 groups of four neighbours.  The logits of the
+// next round of tokens are requested before this one's are worked on, and the first ones before the sequence is looked up.
+// ONE: a single workgroup counts the picks too, in LDS, and needs no other's share.
+template <int GS, int VPL, bool V4, bool ONE>
+__global__ __launch_bounds__(kLossThreads) void seq_loss_kernel(const SeqArgs a) {
     constexpr int TPW = 64 / GS;
-    __shared__ float red[256];
-    __shared__ int last;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ float red[kLossThreads];
+    __shared__ int last, used_one;
+    __shared__ int hist[ONE ? kOneCounts : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int grp = lane / GS, sl = lane % GS;
     const int E = a.E;
     const auto add = [](float x, float y) { return x + y; };
     const auto fmx = [](float x, float y) { return fmaxf(x, y); };
     auto index = [&](int i) { return V4 ? (i / 4) * GS * 4 + sl * 4 + i % 4 : sl + GS * i; };
-    const int per_wave = a.tok_per_block / 4;
-    const int t_first = blockIdx.x * a.tok_per_block + wave * per_wave + grp;
-    const int end = min(a.T, blockIdx.x * a.tok_per_block + (wave + 1) * per_wave);
-    // the sequence that holds a token, or the next one: the first whose end lies behind it
-    int b = 0, s0 = 0, s1 = 0;
-    {
-        int hi = a.n_seq;
-        while (b < hi) {
-            const int mid = (b + hi) >> 1;
-            if (a.offsets[mid + 1] > t_first) hi = mid;
-            else b = mid + 1;
+    const int per_wave = a.tok_per_block / (kLossThreads / 64);
+    const long long block0 = (long long)blockIdx.x * a.tok_per_block;
+    const int t0 = (int)min(block0 + wave * per_wave, (long long)a.T), end = (int)min((long long)t0 + per_wave, (long long)a.T);
+    const float none = a.softmax ? -INFINITY : 0.f;          // past the pool: adds nothing to any sum
+    float zn[VPL];
+    auto fetch = [&](int t) {
+        const float* zr = a.logits + (size_t)min(t, a.T - 1) * E;
+        if constexpr (V4) {
+#pragma unroll
+            for (int i = 0; i < VPL; i += 4) {
+                const f32x4 v = index(i) < E ? *reinterpret_cast<const f32x4*>(zr + index(i)) : f32x4{none, none, none, none};
+#pragma unroll
+                for (int j = 0; j < 4; j++) zn[i + j] = v[j];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < VPL; i++) zn[i] = index(i) < E ? zr[index(i)] : none;
         }
+    };
+    float sum = 0.f;
+    int b = 0, s0 = 0, s1 = 0;
+    if (t0 < end) {
+        fetch(t0 + grp);
+        b = find_sequence(a, t0, lane);
         if (b < a.n_seq) seq_range(a, b, s0, s1);
     }
+    const int n_counts = a.n_seq * E;
+    if constexpr (ONE) {
+        for (int i = threadIdx.x; i < n_counts; i += kLossThreads) hist[i] = 0;
+        if (threadIdx.x == 0) used_one = 0;
+        __syncthreads();
+        for (int i = wave; i < a.n_seq; i += kLossThreads / 64) {          // a wavefront to a sequence
+            int r0, r1;
+            seq_range(a, i, r0, r1);
+            if (lane == 0 && r1 > r0) atomicAdd(&used_one, 1);
+            for (int s = r0 * a.k + lane; s < r1 * a.k; s += 64) {
+                const int e = a.topk_idx[s];
+                if (e >= 0 && e < E) atomicAdd(&hist[i * E + e], 1);
+            }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < n_counts; i += kLossThreads) a.counts[i] = hist[i];
+    }
+    const int* const counts = ONE ? hist : a.counts;
+    const float used = (float)(ONE ? used_one : a.state[0]);
     int have = -1;                                   // the sequence whose coefficients are held
     float coef[VPL];
 #pragma unroll
     for (int i = 0; i < VPL; i++) coef[i] = 0.f;
-    float sum = 0.f;
-    for (int t = t_first; t - grp < end; t += TPW) {                  // the groups of a wavefront stay together
+    for (int tw = t0; tw < end; tw += TPW) {
+        const int t = tw + grp;
         const bool live = t < end;
-        const int tc = min(t, a.T - 1);
         while (b < a.n_seq && s1 <= t) {
             b++;
             if (b < a.n_seq) seq_range(a, b, s0, s1);
@@ -124,34 +186,24 @@ __global__ __launch_bounds__(256) void seq_loss_kernel(const SeqArgs a) {
         if (in && have != b) {
             have = b;
             const float len = (float)(s1 - s0);
-            const float w = a.alpha * (float)E / ((float)a.k * len * len * (float)a.state[0]);
+            const float w = a.alpha * (float)E / ((float)a.k * len * len * used);
 #pragma unroll
-            for (int i = 0; i < VPL; i++) coef[i] = index(i) < E ? w * (float)a.counts[(size_t)b * E + index(i)] : 0.f;
+            for (int i = 0; i < VPL; i++) coef[i] = index(i) < E ? w * (float)counts[(size_t)b * E + index(i)] : 0.f;
         }
-        const float* zr = a.logits + (size_t)tc * E;
         float z[VPL], dz[VPL];
-        if constexpr (V4) {
 #pragma unroll
-            for (int i = 0; i < VPL; i += 4) {
-                const f32x4 v = index(i) < E ? *reinterpret_cast<const f32x4*>(zr + index(i)) : f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int j = 0; j < 4; j++) z[i + j] = v[j];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < VPL; i++) z[i] = index(i) < E ? zr[index(i)] : 0.f;
-        }
+        for (int i = 0; i < VPL; i++) z[i] = zn[i];
+        if (tw + TPW < end) fetch(tw + TPW + grp);
         float part = 0.f;
         if (a.softmax) {
-            float zmax = -INFINITY;
+            float zmax = z[0];
 #pragma unroll
-            for (int i = 0; i < VPL; i++)
-                if (index(i) < E) zmax = fmaxf(zmax, z[i]);
+            for (int i = 1; i < VPL; i++) zmax = fmaxf(zmax, z[i]);
             zmax = group_reduce_f<GS>(zmax, fmx);
             float se = 0.f;
 #pragma unroll
             for (int i = 0; i < VPL; i++) {
-                z[i] = index(i) < E ? expf(z[i] - zmax) : 0.f;
+                z[i] = __expf(z[i] - zmax);           // off by 2^-24 of the exponent, so of small probabilities only
                 se += z[i];
             }
             se = group_reduce_f<GS>(se, add);
@@ -203,18 +255,29 @@ __global__ __launch_bounds__(256) void seq_loss_kernel(const SeqArgs a) {
     if (lane == 0) red[wave] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
-        const float v = ((red[0] + red[1]) + red[2]) + red[3];
-        __hip_atomic_store(&a.loss_part[blockIdx.x], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        last = __hip_atomic_fetch_add(&a.state[1], 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+        float v = 0.f;
+        for (int w = 0; w < kLossThreads / 64; w++) v += red[w];
+        if constexpr (ONE) {
+            a.loss[0] = v;
+            if (a.d_sigma != nullptr) a.d_sigma[0] = a.softmax ? 0.f : v / a.sigma;
+            return;
+        }
+        // The exchange returns when the share has reached memory, where all XCDs see it; only then is the arrival counted.  An
+        // arrival with release order instead would write the whole L2 back, once per workgroup (16384 tokens of 512 experts: 53 us).
+        const float old = __hip_atomic_exchange(&a.loss_part[blockIdx.x], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        int one = 1;
+        asm volatile("" : "+v"(one) : "v"(old) : "memory");
+        last = __hip_atomic_fetch_add(&a.state[1], one, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
     }
+    if constexpr (ONE) return;
     __syncthreads();
     if (!last) return;
     float v = 0.f;
-    for (int i = threadIdx.x; i < (int)gridDim.x; i += 256)
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += kLossThreads)
         v += __hip_atomic_load(&a.loss_part[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     red[threadIdx.x] = v;
     __syncthreads();
-    for (int s = 128; s > 0; s >>= 1) {
+    for (int s = kLossThreads / 2; s > 0; s >>= 1) {
         if (threadIdx.x < s) red[threadIdx.x] += red[threadIdx.x + s];
         __syncthreads();
     }
@@ -237,14 +300,22 @@ hipError_t launch_seq_balance_loss(const unipool_shape& s, int n_seq, const int3
     a.parts = (long long)n_seq * kTokensPerPart <= s.T ? std::min(cdiv(s.T, n_seq * kTokensPerPart), 1024) : 1;
     a.alpha = alpha; a.sigma = s.sigma; a.c = s.c; a.eps = s.eps;
     a.softmax = s.router == UNIPOOL_ROUTER_SOFTMAX;
-    a.tok_per_block = std::max(dz_tokens_per_block(s), 16);
-    seq_count_kernel<<<dim3(n_seq, a.parts), 256, 0, st>>>(a);
-    if (a.parts > 1) seq_count_sum_kernel<<<(unsigned)(((size_t)n_seq * s.E + 255) / 256), 256, 0, st>>>(a);
+    a.tok_per_block = kLossTokens * cdiv(cdiv(s.T, kLossTokens), kLossBlocks);      // (a word per 64 tokens at most in loss_part)
+    // A few tokens go in one launch instead of two (128 tokens, 8 experts 8.1 -> 5.2 us on the device)
+    const bool one = s.T <= kOneTokens && (long long)n_seq * s.E <= kOneCounts;
+    if (one) {
+        a.tok_per_block = kLossTokens * cdiv(s.T, kLossTokens);
+    } else {
+        seq_count_kernel<<<dim3(n_seq, a.parts), kCountThreads, 0, st>>>(a);
+        if (a.parts > 1) seq_count_sum_kernel<<<(unsigned)(((size_t)n_seq * s.E + 255) / 256), 256, 0, st>>>(a);
+    }
     const bool v4 = s.E % 4 == 0 && (((uintptr_t)logits | (uintptr_t)d_logits) & 15) == 0;
     const int grid = cdiv(s.T, a.tok_per_block);
     auto run = [&](auto gs, auto vpl) {
-        if (v4) seq_loss_kernel<gs(), vpl(), true><<<grid, 256, 0, st>>>(a);
-        else seq_loss_kernel<gs(), vpl(), false><<<grid, 256, 0, st>>>(a);
+        if (one && v4) seq_loss_kernel<gs(), vpl(), true, true><<<1, kLossThreads, 0, st>>>(a);
+        else if (one) seq_loss_kernel<gs(), vpl(), false, true><<<1, kLossThreads, 0, st>>>(a);
+        else if (v4) seq_loss_kernel<gs(), vpl(), true, false><<<grid, kLossThreads, 0, st>>>(a);
+        else seq_loss_kernel<gs(), vpl(), false, false><<<grid, kLossThreads, 0, st>>>(a);
     };
     using std::integral_constant;
     if (s.E <= 64) run(integral_constant<int, 16>{}, integral_constant<int, 4>{});

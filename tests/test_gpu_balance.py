@@ -84,7 +84,7 @@ def test_loss_counts_and_gradients(T, E, k, router):
         check(T, E, k, router, z, off, run(T, E, k, router, z, picks(z, k), off))
 
 
-@pytest.mark.parametrize("T,n_seq", [(16384, 1), (9000, 2), (4096, 1), (4095, 1)])
+@pytest.mark.parametrize("T,n_seq", [(16384, 1), (9000, 2), (4096, 1), (4095, 1), (40000, 3)])
 def test_long_sequences_are_counted_in_parts(T, n_seq):
     E, k = 8, 2
     z = np.random.default_rng(T).standard_normal((T, E)).astype(np.float32)
@@ -165,3 +165,13 @@ def test_router_backward_takes_the_gradients_in(dtype, T, d, E, k, router):
     assert rel_err(dx, dx_own + dz_ref @ w) <= TOL[dtype]
     total = np.asarray(ds_own).reshape(-1)[0] + ds_ref
     assert abs(dsig[0] - total) <= 1e-5 * max(abs(total), np.abs(dgate).sum())
+
+
+@pytest.mark.parametrize("T,E,n_seq", [(256, 32, 256), (257, 32, 256), (256, 33, 256), (256, 512, 16), (256, 512, 17), (100, 8, 3000)])
+def test_one_workgroup_and_several(T, E, n_seq):
+    """Both sides of the line up to which a single workgroup does everything, and more sequences than tokens."""
+    k = 2
+    z = np.random.default_rng(E + n_seq).standard_normal((T, E)).astype(np.float32)
+    off = np.sort(np.random.default_rng(n_seq).integers(0, T + 1, n_seq + 1)).astype(np.int32)
+    for router in ("norm", "softmax"):
+        check(T, E, k, router, z, off, run(T, E, k, router, z, picks(z, k), off))
