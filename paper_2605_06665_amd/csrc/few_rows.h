@@ -81,6 +81,43 @@ __device__ __forceinline__ void few_reduce(const bf16* const (&wp)[NF], size_t h
         if (s + u < ns) multiply(u);
 }
 
+// Experts with rows in ascending order, found by a workgroup of WAVES wavefronts: expert, first row and rows.  Returns how many.
+// One pass over the offsets, which costs less than the launch that a table would need.  e, r0, n: kMaxE words each.
+template <int WAVES>
+__device__ __forceinline__ int few_experts(const int32_t* offsets, int E, int* list_e, int* list_r0, int* list_n) {
+    constexpr int kThreads = 64 * WAVES;
+    __shared__ int wcnt[kMaxE / kThreads][WAVES];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int n_list = 0;
+#pragma unroll
+    for (int p = 0; p < kMaxE / kThreads; p++) {
+        const int e = p * kThreads + tid;
+        int r0 = 0, n = 0;
+        if (e < E) {
+            r0 = offsets[e];
+            n = offsets[e + 1] - r0;
+        }
+        const unsigned long long has = __ballot(n > 0);
+        if (lane == 0) wcnt[p][wave] = __popcll(has);
+        __syncthreads();
+        int at = n_list;
+#pragma unroll
+        for (int w = 0; w < WAVES; w++) {
+            if (w < wave) at += wcnt[p][w];
+            n_list += wcnt[p][w];
+        }
+        if (n > 0) {
+            at += __popcll(has & ((1ull << lane) - 1ull));
+            list_e[at] = e;
+            list_r0[at] = r0;
+            list_n[at] = n;
+        }
+    }
+    __syncthreads();
+    return n_list;
+}
+
 }  // namespace
 
 }  // namespace unipool

@@ -16,8 +16,7 @@
 //     21.6 us);
 //   * activation fragments (the B operand) come the same way, up to 32 rows per pass over the weights; rows past
 //     the expert's last repeat it, so they add no cache lines.
-// Every workgroup finds the experts with rows by itself (one pass over the offsets), which costs less than
-// the launch that a table would need.
+// Every workgroup finds the experts with rows by itself (few_experts).
 // Measured, both products (launches back to back in a graph), against the tiles of gemm_xw: 192 experts of 1536 x 4096,
 // k = 2: 1 token 54 -> 20 us, 4 tokens 93 -> 52 (5.7 TB/s), 64 tokens 662 -> 575; 512 experts of 1024 x 704, k = 8, 48
 // tokens 250 -> 188 us (6.2 TB/s); pools that fit the caches: 32 experts of 512 x 512, k = 2, 64 tokens 23 -> 15 us, 16
@@ -27,8 +26,6 @@
 namespace unipool {
 
 namespace {
-
-constexpr int kFewMaxE = 512;
 
 struct FewArgs {
     const bf16* X;                      // [rows][K], or the tokens when gather is given
@@ -89,38 +86,10 @@ __device__ __forceinline__ void few_task(const FewArgs& a, const bf16* We, int c
 // RM: most row fragments per pass over an expert's weights, D1 / DM: steps in flight with one / RM fragments
 template <bool GATE_UP, int WAVES, int RM, int D1, int DM>
 __global__ __launch_bounds__(64 * WAVES) void ffn_few_kernel(const FewArgs a) {
-    constexpr int kThreads = 64 * WAVES;
-    __shared__ int list_e[kFewMaxE], list_r0[kFewMaxE], list_n[kFewMaxE];
-    __shared__ int wcnt[kFewMaxE / kThreads][WAVES];
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // experts with rows, in ascending order
-    int n_list = 0;
-#pragma unroll
-    for (int p = 0; p < kFewMaxE / kThreads; p++) {
-        const int e = p * kThreads + tid;
-        int r0 = 0, n = 0;
-        if (e < a.E) {
-            r0 = a.offsets[e];
-            n = a.offsets[e + 1] - r0;
-        }
-        const unsigned long long has = __ballot(n > 0);
-        if (lane == 0) wcnt[p][wave] = __popcll(has);
-        __syncthreads();
-        int at = n_list;
-#pragma unroll
-        for (int w = 0; w < WAVES; w++) {
-            if (w < wave) at += wcnt[p][w];
-            n_list += wcnt[p][w];
-        }
-        if (n > 0) {
-            at += __popcll(has & ((1ull << lane) - 1ull));
-            list_e[at] = e;
-            list_r0[at] = r0;
-            list_n[at] = n;
-        }
-    }
-    __syncthreads();
+    __shared__ int list_e[kMaxE], list_r0[kMaxE], list_n[kMaxE];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int n_list = few_experts<WAVES>(a.offsets, a.E, list_e, list_r0, list_n);
     const int per_e = a.N / 16;
     const int tasks = n_list * per_e;
     for (int t = blockIdx.x * WAVES + wave; t < tasks; t += gridDim.x * WAVES) {
