@@ -524,6 +524,8 @@ int unipool_expert_ffn_fwd_mx8(const unipool_shape* shape, const void* x_q, cons
     PROLOGUE();
     if (shape->dtype != UNIPOOL_BF16)
         return set_error(UNIPOOL_EINVAL, "%s: experts in 8 bits exist in bfloat16 mode only", __func__);
+    if (shape->d_model > (1 << 20) || shape->d_ff > (1 << 20))
+        return set_error(UNIPOOL_EINVAL, "%s: d_model and d_ff must be at most 2^20 (d=%d f=%d)", __func__, shape->d_model, shape->d_ff);
     REQUIRE_PTR(x_q); REQUIRE_PTR(x_scale); REQUIRE_PTR(expert_offsets); REQUIRE_PTR(w_gate_up_q); REQUIRE_PTR(w_gate_up_scale);
     REQUIRE_PTR(w_down_q); REQUIRE_PTR(w_down_scale); REQUIRE_PTR(h_q); REQUIRE_PTR(h_scale); REQUIRE_PTR(y_perm);
     if (!aligned(x_q, 16) || !aligned(w_gate_up_q, 16) || !aligned(w_down_q, 16) || !aligned(h_q, 16) || !aligned(y_perm, 16))

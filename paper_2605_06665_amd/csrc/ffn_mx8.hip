@@ -80,21 +80,69 @@ __device__ __forceinline__ void glds4(const void* gptr, unsigned lds_addr) {
                  : "memory", "m0");
 }
 
+// The tiles of a workgroup in the order of TileWalk, 64 at a time: lane i holds the tile of round base + i, so the divisions and the table
+// reads of a tile are done once for 64 of them.
+struct TileList {
+    int next, base;                  // round that comes next; round of lane 0
+    int rows, expert, row0, nt;      // per lane; rows: 0 a place without a tile, -1 past the end
+};
+__device__ __forceinline__ void tiles_at(TileList& l, const GemmArgs& g, int round0, int lane) {
+    const int n_mt = g.tile_meta[0], G = g.group_m, per_group = G * g.n_tiles_n;
+    const int total = ((n_mt + G - 1) / G) * per_group, per_xcd = (total + kNumXcd - 1) / kNumXcd;
+    const int xcd = blockIdx.x % kNumXcd, slot = blockIdx.x / kNumXcd, P = gridDim.x / kNumXcd;
+    const int round = round0 + lane, lt = xcd * per_xcd + round * P + (slot + round) % P;
+    l.next = l.base = round0;
+    l.rows = l.expert = l.row0 = l.nt = 0;
+    if (lt >= min(total, (xcd + 1) * per_xcd)) {
+        l.rows = -1;
+        return;
+    }
+    const int rem = lt % per_group, mt = lt / per_group * G + rem % G;
+    if (mt >= n_mt) return;
+    const int4 m = *reinterpret_cast<const int4*>(g.tile_meta + kTileBase + 4 * mt);
+    l.expert = m.x;
+    l.row0 = m.y;
+    l.rows = max(m.z, 0);
+    l.nt = rem / G;
+}
+__device__ __forceinline__ TileRef next_tile(TileList& l, const GemmArgs& g, int lane) {
+    TileRef t = {0, 0, 0, 0, 0, -1};
+    for (;;) {
+        if (l.next - l.base == 64) tiles_at(l, g, l.next, lane);
+        const int i = l.next - l.base;
+        const int rows = __builtin_amdgcn_readlane(l.rows, i);
+        if (rows < 0) return t;
+        l.next++;
+        if (rows == 0) continue;
+        t.valid = 1;
+        t.rows = rows;
+        t.expert = __builtin_amdgcn_readlane(l.expert, i);
+        t.row0 = __builtin_amdgcn_readlane(l.row0, i);
+        t.nt = __builtin_amdgcn_readlane(l.nt, i);
+        return t;
+    }
+}
+
 // Tile of BM rows by 256 weight rows (gate-up: 128 gate rows and the 128 up rows they meet), eight wavefronts: wavefront (wm, wn)
-// owns 64 weight rows and every second fragment of 16 rows starting at wm.  Fragments without rows are skipped.
+// owns 64 weight rows and every second fragment of 16 rows starting at wm.  Fragments without rows are multiplied like the others: the tile's time
+// is that of its loads, and one straight body keeps the accumulators where they are (a body per number of fragments, as alternatives of one
+// switch, had the compiler move and spill them).
 //
-// A workgroup is persistent and its tiles form one stream of stages of 128 indices: while a stage is multiplied, the next ones land
-// in rings of LDS buffers (NSX of rows, NSW of weights and scales), whatever tile they belong to, so a tile starts with its first
-// stages in place and its epilogue runs beside the loads of the next.  A wavefront waits for its own loads of the next stage
-// and meets the others once per stage; the buffers that the meeting frees are filled by the loads that are spread over the next stage.
+// A workgroup is persistent and its tiles form one stream of stages of 128 indices, whatever tile they belong to: rings of LDS buffers
+// (NSX of rows, NSW of weights and scales) are filled ahead across tiles, so a tile starts with its first stages in place and its
+// epilogue runs beside the loads of the next.
+// A stage has two parts.  In the first the wavefront multiplies all but its last two fragments, fetching the rows' fragments two ahead, while
+// the loads of weights go out that fill the buffer the stage before has released.  Then the wavefronts meet: everyone's loads of the next stage have landed and nobody reads
+// this one any more.  The second part multiplies the last two fragments from registers, and while it does the weights' fragments are replaced
+// by the next stage's, the next stage's first rows are fetched, and the loads of rows go out into the buffer that has become free.
 template <bool GATE_UP, int BM, int NSX, int NSW> struct Mx8Tile {
     static constexpr int BN = 256, NW = 8, ROWB = kMxStep;
     static constexpr int XBYTES = BM * ROWB, WBYTES = BN * ROWB, SBYTES = (BN + BM) * 4;
     static constexpr int XI = XBYTES / (NW * 1024), WI = WBYTES / (NW * 1024);      // 1 KB loads of a wavefront
     static constexpr int MF = BM / 32;                    // fragments of a wavefront
-    static constexpr int WBASE = NSX * XBYTES, SBASE = WBASE + NSW * WBYTES;
-    static constexpr int LDS = SBASE + NSW * SBYTES;
-    static_assert(LDS <= 160 * 1024 && NSX >= 2 && NSX <= NSW, "the rings fit a compute unit");
+    static constexpr int WBASE = NSX * XBYTES, SBASE = WBASE + NSW * WBYTES, GBASE = SBASE + NSW * SBYTES;
+    static constexpr int LDS = GBASE + 2 * BM * 4;
+    static_assert(LDS <= 160 * 1024 && NSX >= 2 && NSW == 3 && NSX <= NSW, "the rings fit a compute unit");
     static constexpr int COLS = GATE_UP ? BN / 2 : BN;    // output columns
 };
 
@@ -107,163 +155,257 @@ __global__ __launch_bounds__(512, 2) void ffn_mx8_kernel(const Mx8Args a) {
     const int l16 = lane & 15, lg = lane >> 4, wm = wave & 1, wn = wave >> 1;
     const unsigned lds0 = lds_addr_of(smem);
     const int nk = (a.K + kMxStep - 1) / kMxStep;
-    const char* const zeros = reinterpret_cast<const char*>(g_mx8_zero_page);
+    const bool half = a.K % kMxStep != 0;                  // the last stage of a tile has 64 indices
     // 16-byte piece ch of a row lies at place ch ^ ((row / 2) & 7) of its 128 bytes, so that 16 rows' pieces lie in different banks
     auto swz = [](int row) { return (row >> 1) & 7; };
 
-    // ---- load cursors: the stages of rows run NSX - 1 ahead of the multiplication, those of weights and scales NSW - 1 -------------
-    TileWalk xwalk(a.g), wwalk(a.g);
+    // ---- load cursors ---------------------------------------------------------------------------------------
+    TileList xlist, wlist;
+    tiles_at(xlist, a.g, 0, lane);
+    wlist = xlist;
+    TileList clist = xlist;
     bool xon, won;
-    int xkt = 0, wkt = 0, xbuf = 0, wbuf = 0;
-    const char *xsrc[XI], *wsrc[WI], *ssrc;
-    // (loads 8 rows apart differ by whole rows: the piece a lane fetches is the same in all of them)
-    const int piece = ((lane & 7) ^ swz(wave * 8 + (lane >> 3))) * 16;
-    const long long sstep = wave < 4 ? (long long)a.E * a.w_rows * 4 : a.x_rows * 4;
-    auto row_of = [&](const TileRef& t, int r) {
+    int xkt = 0, wkt = 0, xtile = -1, wtile = -1;
+    unsigned xdst = 0, wdst = 0, sdst = 0;                 // ring places, in bytes
+    const char *xsrc[XI], *wbase, *ssrc;
+    constexpr int WV = GATE_UP ? WI / 2 : WI;              // gate and up rows of a lane lie at the same offsets from their first rows
+    unsigned woff[WV];
+    // (loads 64 rows apart have the same piece in a lane)
+    auto piece_of = [&](int ln) { return ((ln & 7) ^ swz(wave * 8 + (ln >> 3))) * 16; };
+    const bool upper = piece_of(lane) >= 64;               // absent from a stage of 64 indices: zeros
+    const char* const zeros = reinterpret_cast<const char*>(g_mx8_zero_page);
+    long long xinc = kMxStep, winc = kMxStep, sinc = wave < 4 ? (long long)a.E * a.w_rows * 4 : a.x_rows * 4;      // from stage to stage
+    // Rows of a gathered tile are looked up while the tile before is loaded: their numbers pass through LDS (two tiles' worth), since a wait
+    // for a load to a register would wait for every stage in flight.  They are there two stages later: tiles of one or two are too short.
+    const bool by_lds = a.gather != nullptr && nk >= 3;
+    bool prologue = true;
+    auto row_of = [&](const TileRef& t, int r, int tile) {
         const int row = t.row0 + min(r, t.rows - 1);
-        return (long long)(a.gather ? a.gather[row] / a.gather_div : row);
+        if (a.gather == nullptr) return (long long)row;
+        const int slot = by_lds && !prologue ? *reinterpret_cast<const int*>(smem + C::GBASE + ((tile & 1) * BM + min(r, t.rows - 1)) * 4)
+                                             : a.gather[row];
+        return (long long)(slot / a.gather_div);
     };
     auto weight_of = [&](const TileRef& t, int r) {
         const int n0 = t.nt * C::COLS;
         const int c = GATE_UP ? min(n0 + (r & (BN / 2 - 1)), a.N - 1) + (r / (BN / 2)) * a.N : min(n0 + r, a.N - 1);
         return (long long)t.expert * a.w_rows + c;
     };
+    // (in what follows the lane number is made opaque, or what depends on it alone would be kept in registers across the stages)
     auto next_x = [&]() {
-        const TileRef t = xwalk.next(a.g);
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        const TileRef t = next_tile(xlist, a.g, ln);
         xon = t.valid;
         xkt = 0;
-        if (!xon) return;
+        xtile++;
+        if (!xon) {                                        // past the last tile the loads go on, from the page of zeros
+            xinc = 0;
 #pragma unroll
-        for (int i = 0; i < XI; i++)
-            xsrc[i] = reinterpret_cast<const char*>(a.x) + row_of(t, (i * C::NW + wave) * 8 + (lane >> 3)) * a.K + piece;
+            for (int i = 0; i < XI; i++) xsrc[i] = zeros;
+            return;
+        }
+        const int r = wave * 8 + (ln >> 3), at = piece_of(ln);
+#pragma unroll
+        for (int i = 0; i < XI; i++) xsrc[i] = reinterpret_cast<const char*>(a.x) + row_of(t, i * C::NW * 8 + r, xtile) * a.K + at;
     };
+    TileRef wnext = next_tile(wlist, a.g, lane);
+    if (!wnext.valid) return;                              // no tile for this workgroup
     auto next_w = [&]() {
-        const TileRef t = wwalk.next(a.g);
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        const TileRef t = wnext;
         won = t.valid;
         wkt = 0;
-        if (!won) return;
+        wtile++;
+        if (!won) {
+            winc = sinc = 0;
+            wbase -= kMxStep;
+            ssrc = zeros;                                  // (the weights' loads repeat the last stage)
+            wkt = nk - 1;
+            return;
+        }
+        const int r = wave * 8 + (ln >> 3), at = piece_of(ln);
 #pragma unroll
-        for (int i = 0; i < WI; i++)
-            wsrc[i] = reinterpret_cast<const char*>(a.w) + weight_of(t, (i * C::NW + wave) * 8 + (lane >> 3)) * a.K + piece;
+        for (int i = 0; i < WV; i++) woff[i] = (unsigned)min(i * C::NW * 8 + r, a.N - 1 - t.nt * C::COLS) * (unsigned)a.K + at;
+        wbase = reinterpret_cast<const char*>(a.w) + ((long long)t.expert * a.w_rows + t.nt * C::COLS) * a.K;
         // scales: one load a wavefront, of 64 weight rows or 64 rows (some of them twice where there are fewer)
-        if (wave < 4) ssrc = reinterpret_cast<const char*>(a.w_scale) + weight_of(t, wave * 64 + lane) * 4;
-        else ssrc = reinterpret_cast<const char*>(a.x_scale) + row_of(t, (wave - 4) % (BM / 64) * 64 + lane) * 4;
+        if (wave < 4) ssrc = reinterpret_cast<const char*>(a.w_scale) + weight_of(t, wave * 64 + ln) * 4;
+        else ssrc = reinterpret_cast<const char*>(a.x_scale) + row_of(t, (wave - 4) % (BM / 64) * 64 + ln, wtile) * 4;
+        wnext = next_tile(wlist, a.g, ln);
+        if (by_lds && wnext.valid && wave < BM / 64)
+            glds4(a.gather + wnext.row0 + min(wave * 64 + ln, wnext.rows - 1), lds0 + C::GBASE + (((wtile + 1) & 1) * BM + wave * 64) * 4);
     };
-    const unsigned sdst = lds0 + C::SBASE + (wave < 4 ? wave * 256 : BN * 4 + (wave - 4) % (BM / 64) * 256);
-    // load i of the cursors' stages: first the rows, then the weights, last the scales
-    auto issue = [&](int i) {
-        if (i < XI) {
-            if (xon) {
-                const char* src = xkt * kMxStep + piece < a.K ? xsrc[i < XI ? i : 0] + (size_t)xkt * kMxStep : zeros;
-                glds16(src, lds0 + xbuf * C::XBYTES + (i * C::NW + wave) * 1024);
-            }
-        } else if (i < XI + WI) {
-            const int u = i - XI;
-            if (won) {
-                const char* src = wkt * kMxStep + piece < a.K ? wsrc[u >= 0 && u < WI ? u : 0] + (size_t)wkt * kMxStep : zeros;
-                glds16(src, lds0 + C::WBASE + wbuf * C::WBYTES + (u * C::NW + wave) * 1024);
-            }
-        } else if (won) {
-            glds4(ssrc + wkt * sstep, sdst + wbuf * C::SBYTES);
+    const unsigned sbase = lds0 + C::SBASE + (wave < 4 ? wave * 256 : BN * 4 + (wave - 4) % (BM / 64) * 256);
+    auto issue_x = [&](int i) {
+        const char* src = half && xkt == nk - 1 && upper ? zeros : xsrc[i];
+        glds16(src, lds0 + xdst + (i * C::NW + wave) * 1024);
+        xsrc[i] += xinc;
+    };
+    const long long up = (long long)a.N * a.K;             // from a gate row to its up row
+    auto issue_w = [&](int i) {                            // i == WI: the scales
+        if (i < WI) {
+            // (in a stage of 64 indices the absent pieces are those of the first half again: they meet zeros)
+            const unsigned at = woff[i % WV] - (half && wkt == nk - 1 && upper ? 64 : 0);
+            glds16_s(wbase + (i / WV) * up, at, lds0 + C::WBASE + wdst + (i * C::NW + wave) * 1024);
+        } else {
+            glds4(ssrc, sbase + sdst);
+            ssrc += sinc;
+            wbase += winc;
         }
     };
-    constexpr int NL = XI + WI + 1;
     auto advance_x = [&]() {
-        xbuf = xbuf + 1 == NSX ? 0 : xbuf + 1;
+        xdst = xdst + C::XBYTES == NSX * C::XBYTES ? 0 : xdst + C::XBYTES;
         if (xon && ++xkt == nk) next_x();
     };
     auto advance_w = [&]() {
-        wbuf = wbuf + 1 == NSW ? 0 : wbuf + 1;
+        wdst = wdst + C::WBYTES == NSW * C::WBYTES ? 0 : wdst + C::WBYTES;
+        sdst = sdst + C::SBYTES == NSW * C::SBYTES ? 0 : sdst + C::SBYTES;
         if (won && ++wkt == nk) next_w();
     };
     next_x();
     next_w();
+#pragma unroll
+    for (int s = 0; s < NSX; s++) {
+#pragma unroll
+        for (int i = 0; i < XI; i++) issue_x(i);
+        advance_x();
+    }
+#pragma unroll
     for (int s = 0; s < NSW - 1; s++) {
-        if (s < NSX - 1) {
 #pragma unroll
-            for (int i = 0; i < XI; i++) issue(i);
-            advance_x();
-        }
-#pragma unroll
-        for (int i = XI; i < NL; i++) issue(i);
+        for (int i = 0; i <= WI; i++) issue_w(i);
         advance_w();
     }
+    prologue = false;
     wait_vmcnt<0>();
     lds_barrier();
 
+    // ---- fragments --------------------------------------------------------------------------------------------
+    // ring places of the stage that is multiplied; lane addresses: a base per ring, the fragment in the instruction's offset
+    unsigned xo = 0, wo = 0, so = 0;
+    const int p0 = (lg ^ swz(l16)) * 16, p1 = ((4 + lg) ^ swz(l16)) * 16;
+    const unsigned lx = (wm * 16 + l16) * C::ROWB, lsx = C::SBASE + (BN + wm * 16 + l16) * 4 + lg;
+    const unsigned lw = C::WBASE + (wn * (GATE_UP ? 32 : 64) + l16) * C::ROWB, lsw = C::SBASE + (wn * (GATE_UP ? 32 : 64) + l16) * 4 + lg;
+    i32x8 wf[4], xf[3];                                    // fragment m of the rows in registers m mod 3
+    int wsb[4], xsb[3];
+    auto load_w = [&](int n, unsigned w_at, unsigned s_at) {
+        constexpr int kHalf = GATE_UP ? BN / 2 : 32;
+        const int r = (n >> 1) * kHalf + (n & 1) * 16;
+        wf[n] = two16(*reinterpret_cast<const uint4*>(smem + lw + p0 + w_at + r * C::ROWB), *reinterpret_cast<const uint4*>(smem + lw + p1 + w_at + r * C::ROWB));
+        wsb[n] = *reinterpret_cast<const unsigned char*>(smem + lsw + s_at + r * 4);
+    };
+    auto load_x = [&](int b, int m, unsigned x_at, unsigned s_at) {      // fragment m into registers b
+        xf[b] = two16(*reinterpret_cast<const uint4*>(smem + lx + p0 + x_at + m * 32 * C::ROWB),
+                      *reinterpret_cast<const uint4*>(smem + lx + p1 + x_at + m * 32 * C::ROWB));
+        xsb[b] = *reinterpret_cast<const unsigned char*>(smem + lsx + s_at + m * 32 * 4);
+    };
+    const bool upper_half = lg >= 2;
+#pragma unroll
+    for (int n = 0; n < 4; n++) load_w(n, 0, 0);
+    load_x(0, 0, 0, 0);
+    load_x(1, 1, 0, 0);
+
+    // ---- a stage ------------------------------------------------------------------------------------------
+    f32x4 acc[MF][4];
+    auto stage = [&](int kt) {
+        constexpr int H = 2, M1 = MF - H;                   // fragments of the second and of the first part
+        const bool tail = half && kt == nk - 1 && upper_half;
+        auto mfma = [&](int m, int n) {
+            const int b = m % 3;
+            // past the end of K the values are zeros; their scales must not be NaN
+            if (m == 0) wsb[n] = tail ? kMxBias : wsb[n];
+            if (n == 0) xsb[b] = tail ? kMxBias : xsb[b];
+            acc[m][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf[n], xf[b], acc[m][n], 0, 0, 0, wsb[n], 0, xsb[b]);
+        };
+        // Products stay where they are written: moved behind the meeting or the change of tiles they would keep the fragments of two stages in
+        // registers.
+        auto keep = [&](int m0, int m1) {
+#pragma unroll
+            for (int m = m0; m < m1; m++)
+#pragma unroll
+                for (int n = 0; n < 4; n++) asm volatile("" : "+v"(acc[m][n]));
+        };
+        // first part
+        constexpr int SL = 4 * M1;
+        if constexpr (SL == 0) {
+#pragma unroll
+            for (int u = 0; u <= WI; u++) issue_w(u);
+        }
+#pragma unroll
+        for (int sl = 0; sl < SL; sl++) {
+            const int m = sl >> 2, n = sl & 3;
+            mfma(m, n);
+            if (n == 0) load_x((m + 2) % 3, m + 2, xo, so);
+#pragma unroll
+            for (int u = 0; u <= WI; u++)
+                if (u * SL / (WI + 1) == sl) issue_w(u);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        keep(0, M1);
+        // the loads of the next stage have landed: only what was issued behind them may be outstanding
+        wait_vmcnt<NSX == NSW ? XI + WI + 1 : WI + 1>();
+        lds_barrier();
+        xo = xo + C::XBYTES == NSX * C::XBYTES ? 0 : xo + C::XBYTES;
+        wo = wo + C::WBYTES == NSW * C::WBYTES ? 0 : wo + C::WBYTES;
+        so = so + C::SBYTES == NSW * C::SBYTES ? 0 : so + C::SBYTES;
+        // second part; registers 0 and 1 take the next stage's rows at once if the last two fragments are not in them
+        auto free_early = [](int b) { return b != M1 % 3 && b != (M1 + 1) % 3; };
+#pragma unroll
+        for (int n = 0; n < 4; n++) {
+#pragma unroll
+            for (int j = 0; j < H; j++) {
+                mfma(M1 + j, n);
+                if (n * H + j < XI) issue_x(n * H + j < XI ? n * H + j : 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            load_w(n, wo, so);
+            if (n < 2 && free_early(n)) load_x(n, n, xo, so);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int n = 0; n < 2; n++)
+            if (!free_early(n)) load_x(n, n, xo, so);
+        keep(M1, MF);
+    };
     // ---- the tiles ------------------------------------------------------------------------------------------
-    TileWalk walk(a.g);
-    int cx = 0, cw = 0;                                    // ring places of the stage that is multiplied
-    const int woff = l16 * C::ROWB, p0 = (lg ^ swz(l16)) * 16, p1 = ((4 + lg) ^ swz(l16)) * 16;
-    for (TileRef t = walk.next(a.g); t.valid; t = walk.next(a.g)) {
-        const int n0 = t.nt * C::COLS;
-        const int col = n0 + wn * (GATE_UP ? 32 : 64);     // the wavefront's columns are inside N or outside as a whole
+    for (;;) {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        const TileRef t = next_tile(clist, a.g, ln);
+        if (!t.valid) break;
+        const int col = t.nt * C::COLS + wn * (GATE_UP ? 32 : 64);       // the wavefront's columns are inside N or outside as a whole
         const int mi = col < a.N ? (((t.rows + 15) >> 4) - wm + 1) >> 1 : 0;
-        f32x4 acc[MF][4];
 #pragma unroll
         for (int m = 0; m < MF; m++)
 #pragma unroll
             for (int n = 0; n < 4; n++) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
         for (int kt = 0; kt < nk; kt++) {
-            const char* xb = smem + cx * C::XBYTES;
-            const char* wb = smem + C::WBASE + cw * C::WBYTES;
-            const unsigned char* sb = reinterpret_cast<const unsigned char*>(smem) + C::SBASE + cw * C::SBYTES;
-            // past the end of K the values are zeros; their scales must not be NaN
-            const bool tail = kt * kMxStep + lg * kMxBlock >= a.K;
-            i32x8 wf[4];
-            int wsb[4];
-#pragma unroll
-            for (int n = 0; n < 4; n++) {
-                const int r = GATE_UP ? (n >> 1) * (BN / 2) + wn * 32 + (n & 1) * 16 : wn * 64 + n * 16;
-                const char* p = wb + r * C::ROWB + woff;
-                wf[n] = two16(*reinterpret_cast<const uint4*>(p + p0), *reinterpret_cast<const uint4*>(p + p1));
-                wsb[n] = sb[(r + l16) * 4 + lg];
-            }
-#pragma unroll
-            for (int n = 0; n < 4; n++) wsb[n] = tail ? kMxBias : wsb[n];
-            const bool w_issued = won;
-#pragma unroll
-            for (int m = 0; m < MF; m++) {
-                if (m < mi) {
-                    const int r = (2 * m + wm) * 16;
-                    const char* p = xb + r * C::ROWB + woff;
-                    const i32x8 xf = two16(*reinterpret_cast<const uint4*>(p + p0), *reinterpret_cast<const uint4*>(p + p1));
-                    int xsb = sb[(BN + r + l16) * 4 + lg];
-                    xsb = tail ? kMxBias : xsb;
-#pragma unroll
-                    for (int n = 0; n < 4; n++)
-                        acc[m][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf[n], xf, acc[m][n], 0, 0, 0, wsb[n], 0, xsb);
-                }
-#pragma unroll
-                for (int i = m * NL / MF; i < (m + 1) * NL / MF; i++) issue(i);
-            }
-            advance_x();
+            stage(kt);
             advance_w();
-            // the loads of the next stage have landed: only what was issued behind them may be outstanding
-            if (w_issued) wait_vmcnt<NSX == NSW ? (NSW - 2) * NL : (NSW - 2) * (WI + 1)>();
-            else wait_vmcnt<0>();
-            lds_barrier();
-            cx = cx + 1 == NSX ? 0 : cx + 1;
-            cw = cw + 1 == NSW ? 0 : cw + 1;
+            advance_x();
         }
         // acc[m][n][i] = C[row 16 (2 m + wm) + l16][weight row 16 n + 4 lg + i of the wavefront's 64]
+        asm volatile("" : "+v"(ln));
+        const int r16 = ln & 15, rg = ln >> 4;
 #pragma unroll
         for (int m = 0; m < MF; m++) {
             if (m >= mi) break;
-            const int r = (2 * m + wm) * 16 + l16;
+            const int r = (2 * m + wm) * 16 + r16;
             const bool on = r < t.rows;
             const long long row = t.row0 + r;
             if constexpr (GATE_UP) {
-                store_h(a, acc[m][0], acc[m][1], acc[m][2], acc[m][3], on, row, col, lg);
+                store_h(a, acc[m][0], acc[m][1], acc[m][2], acc[m][3], on, row, col, rg);
             } else {
 #pragma unroll
                 for (int n = 0; n < 4; n++)
                     if (on)
-                        *reinterpret_cast<uint2*>(a.y + row * a.N + col + n * 16 + 4 * lg) =
+                        *reinterpret_cast<uint2*>(a.y + row * a.N + col + n * 16 + 4 * rg) =
                             pack4(acc[m][n][0], acc[m][n][1], acc[m][n][2], acc[m][n][3]);
             }
         }
     }
+    wait_vmcnt<0>();                                       // no load may land in LDS that is someone else's by then
 }
 
 template <bool GATE_UP, int BM, int NSX, int NSW> hipError_t run_tile(Mx8Args a, hipStream_t st) {

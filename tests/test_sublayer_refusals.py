@@ -112,6 +112,9 @@ def test_experts(U):
         call(sh=shape(U, dtype=U.F32))
     with pytest.raises(U.UniPoolError, match="multiples of 64"):
         call(sh=shape(U, d_ff=96))
+    big = shape(U, T=1, E=1, k=1, d_ff=(1 << 20) + 64)
+    with pytest.raises(U.UniPoolError, match="at most 2"):
+        call(sh=big, ws=ws(U, big))
     with pytest.raises(U.UniPoolError, match="workspace is NULL"):
         call(ws=None)
     with pytest.raises(U.UniPoolError, match="64 bytes"):
