@@ -366,7 +366,7 @@ int unipool_quantize_mx8(int dtype, long long rows, int cols, const void* src, v
  * Products of 8-bit values are added in float on the matrix cores.
  * in : x_q, x_scale: the tokens [T, d] in MX8 when slot_of_row is given (row r of the group order is token slot_of_row[r] / k), or the
  *      rows [S, d] in group order when it is NULL;  expert_offsets [E+1];  w_gate_up_q [E, 2 d_ff, d], w_down_q [E, d, d_ff] with
- *      their scales.  The values and y_perm must be aligned to 16 bytes, the scales to 4; d and d_ff are at most 2^20.
+ *      their scales.  The values, the weights' scales and y_perm must be aligned to 16 bytes, the other scales to 4; d, d_ff <= 2^20.
  * out: h_q [S, d_ff], h_scale (H in MX8);  y_perm [S, d] bfloat16.
  */
 int unipool_expert_ffn_fwd_mx8(const unipool_shape* shape, const void* x_q, const void* x_scale, const int32_t* slot_of_row,

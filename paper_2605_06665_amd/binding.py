@@ -126,11 +126,30 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+def _ptrs(*tensors):
+    """_ptr of several tensors: a call a tensor was most of what marshalling took."""
+    out = []
+    for t in tensors:
+        if t is not None and t.__class__ is not int:
+            if not t.is_contiguous():
+                raise UniPoolError("tensor arguments must be contiguous")
+            t = t.data_ptr()
+        out.append(t)
+    return out
+
+
+_STREAM_OF = _DEVICE = None
+
+
 def _current_stream() -> int:
     """Handle of torch's current stream on the current device.  torch.cuda.current_stream() builds a stream object for it:
     2 us a call, a third of what marshalling a call takes (a step of 18 calls and 29 launches 202 -> 151 us)."""
-    import torch
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    global _STREAM_OF, _DEVICE
+    if _STREAM_OF is None:
+        import torch
+        torch.cuda.current_device()          # sets the device up, if nothing has yet
+        _STREAM_OF, _DEVICE = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    return _STREAM_OF(_DEVICE())
 
 
 def _stream(stream) -> Optional[int]:
@@ -280,31 +299,32 @@ def route_bwd_add(shape, x, w_router, logits, topk_idx, dgate, aux_coef, d_logit
                   dx_accumulate, ws, stream=None):
     """route_bwd with d_logits [T, E] and d_sigma_in [1] (float32, either may be None) added to the gradients of logits and sigma."""
     p, n = _ws(ws)
-    _check(load_library().unipool_route_bwd_add(ctypes.byref(shape), _ptr(x), _ptr(w_router), _ptr(logits), _ptr(topk_idx),
-                                                _ptr(dgate), _ptr(aux_coef), _ptr(d_logits), _ptr(d_sigma_in),
-                                                _ptr(d_w_router), _ptr(d_sigma), _ptr(dx), int(bool(dx_accumulate)), p, n,
-                                                _stream(stream)), "unipool_route_bwd_add")
+    _check((_LIB or load_library()).unipool_route_bwd_add(
+        ctypes.byref(shape), *_ptrs(x, w_router, logits, topk_idx, dgate, aux_coef, d_logits, d_sigma_in, d_w_router, d_sigma, dx),
+        int(bool(dx_accumulate)), p, n, _stream(stream)), "unipool_route_bwd_add")
 
 
 def seq_balance_loss(shape, n_seq, seq_offsets, alpha_seq, logits, topk_idx, counts, loss, d_logits, d_sigma, ws, stream=None):
     """Balance loss of a layer over the sequences [seq_offsets[b], seq_offsets[b + 1]) and its gradient; d_logits, d_sigma may be None."""
     p, n = _ws(ws)
-    _check(load_library().unipool_seq_balance_loss(ctypes.byref(shape), int(n_seq), _ptr(seq_offsets), float(alpha_seq), _ptr(logits),
-                                                   _ptr(topk_idx), _ptr(counts), _ptr(loss), _ptr(d_logits), _ptr(d_sigma), p, n,
-                                                   _stream(stream)), "unipool_seq_balance_loss")
+    off, *ptrs = _ptrs(seq_offsets, logits, topk_idx, counts, loss, d_logits, d_sigma)
+    _check((_LIB or load_library()).unipool_seq_balance_loss(ctypes.byref(shape), n_seq, off, alpha_seq, *ptrs, p, n, _stream(stream)),
+           "unipool_seq_balance_loss")
 
 
 def rmsnorm(shape, x, residual, weight, norm_eps, h, y, y_q, y_scale, stream=None):
     """residual, h, y may be None, and y_q with y_scale; y or y_q must be given."""
-    _check(load_library().unipool_rmsnorm(ctypes.byref(shape), _ptr(x), _ptr(residual), _ptr(weight), float(norm_eps), _ptr(h),
-                                          _ptr(y), _ptr(y_q), _ptr(y_scale), _stream(stream)), "unipool_rmsnorm")
+    x, residual, weight, h, y, y_q, y_scale = _ptrs(x, residual, weight, h, y, y_q, y_scale)
+    _check((_LIB or load_library()).unipool_rmsnorm(ctypes.byref(shape), x, residual, weight, norm_eps, h, y, y_q, y_scale,
+                                                    _stream(stream)), "unipool_rmsnorm")
 
 
 def rmsnorm_bwd(shape, h, weight, dy, dh, norm_eps, dx, d_weight, ws, stream=None):
     """dh may be None; dx may be dy or dh."""
     p, n = _ws(ws)
-    _check(load_library().unipool_rmsnorm_bwd(ctypes.byref(shape), _ptr(h), _ptr(weight), _ptr(dy), _ptr(dh), float(norm_eps),
-                                              _ptr(dx), _ptr(d_weight), p, n, _stream(stream)), "unipool_rmsnorm_bwd")
+    h, weight, dy, dh, dx, d_weight = _ptrs(h, weight, dy, dh, dx, d_weight)
+    _check((_LIB or load_library()).unipool_rmsnorm_bwd(ctypes.byref(shape), h, weight, dy, dh, norm_eps, dx, d_weight, p, n,
+                                                        _stream(stream)), "unipool_rmsnorm_bwd")
 
 
 def mx8_scale_shape(rows, cols):
@@ -314,7 +334,7 @@ def mx8_scale_shape(rows, cols):
 
 def quantize_mx8(dtype, rows, cols, src, q, scale, stream=None):
     """src [rows, cols] (dtype F32 or BF16) to e4m3 bytes q [rows, cols] and scales of mx8_scale_shape(rows, cols), both uint8."""
-    _check(load_library().unipool_quantize_mx8(int(dtype), int(rows), int(cols), _ptr(src), _ptr(q), _ptr(scale), _stream(stream)),
+    _check((_LIB or load_library()).unipool_quantize_mx8(dtype, rows, cols, *_ptrs(src, q, scale), _stream(stream)),
            "unipool_quantize_mx8")
 
 
@@ -322,7 +342,6 @@ def expert_ffn_fwd_mx8(shape, x_q, x_scale, slot_of_row, expert_offsets, w_gate_
                        h_q, h_scale, y_perm, ws, stream=None):
     """slot_of_row None: x_q holds the rows in group order instead of the tokens."""
     p, n = _ws(ws)
-    _check(load_library().unipool_expert_ffn_fwd_mx8(ctypes.byref(shape), _ptr(x_q), _ptr(x_scale), _ptr(slot_of_row),
-                                                     _ptr(expert_offsets), _ptr(w_gate_up_q), _ptr(w_gate_up_scale),
-                                                     _ptr(w_down_q), _ptr(w_down_scale), _ptr(h_q), _ptr(h_scale),
-                                                     _ptr(y_perm), p, n, _stream(stream)), "unipool_expert_ffn_fwd_mx8")
+    _check((_LIB or load_library()).unipool_expert_ffn_fwd_mx8(
+        ctypes.byref(shape), *_ptrs(x_q, x_scale, slot_of_row, expert_offsets, w_gate_up_q, w_gate_up_scale, w_down_q, w_down_scale,
+                                    h_q, h_scale, y_perm), p, n, _stream(stream)), "unipool_expert_ffn_fwd_mx8")

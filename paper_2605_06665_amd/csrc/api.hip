@@ -530,8 +530,8 @@ int unipool_expert_ffn_fwd_mx8(const unipool_shape* shape, const void* x_q, cons
     REQUIRE_PTR(w_down_q); REQUIRE_PTR(w_down_scale); REQUIRE_PTR(h_q); REQUIRE_PTR(h_scale); REQUIRE_PTR(y_perm);
     if (!aligned(x_q, 16) || !aligned(w_gate_up_q, 16) || !aligned(w_down_q, 16) || !aligned(h_q, 16) || !aligned(y_perm, 16))
         return set_error(UNIPOOL_EINVAL, "%s: x_q, w_gate_up_q, w_down_q, h_q and y_perm must be aligned to 16 bytes", __func__);
-    if (!aligned(x_scale, 4) || !aligned(w_gate_up_scale, 4) || !aligned(w_down_scale, 4) || !aligned(h_scale, 4))
-        return set_error(UNIPOOL_EINVAL, "%s: scales must be aligned to 4 bytes", __func__);
+    if (!aligned(x_scale, 4) || !aligned(w_gate_up_scale, 16) || !aligned(w_down_scale, 16) || !aligned(h_scale, 4))
+        return set_error(UNIPOOL_EINVAL, "%s: scales must be aligned to 4 bytes, those of the weights to 16", __func__);
     NEED_WS();
     const WsLayout w = ws_layout(*shape);
     return check_hip(mx8_ffn_fwd(*shape, x_q, x_scale, slot_of_row, expert_offsets, w_gate_up_q, w_gate_up_scale, w_down_q,

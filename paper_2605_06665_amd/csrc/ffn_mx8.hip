@@ -50,17 +50,19 @@ __device__ __forceinline__ i32x8 two16(const uint4& a, const uint4& b) {
 __device__ __forceinline__ void store_h(const Mx8Args& a, const f32x4& a0, const f32x4& a1, const f32x4& b0, const f32x4& b1, bool on,
                                         long long row, int col, int lg) {
     float h[8];
-    unsigned mag = 0;
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         h[i] = silu_f(a0[i]) * b0[i];
         h[4 + i] = silu_f(a1[i]) * b1[i];
     }
+    float m = h[0];
 #pragma unroll
-    for (int i = 0; i < 8; i++) mag = max(mag, mx8_mag(h[i]));
-    mag = max(mag, (unsigned)__shfl_xor((int)mag, 16, 64));
-    mag = max(mag, (unsigned)__shfl_xor((int)mag, 32, 64));
-    const int byte = mx8_scale_byte(mag);
+    for (int i = 1; i < 8; i++) m = mx8_max(m, h[i]);
+    const auto r16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+    m = mx8_max(__uint_as_float(r16[0]), __uint_as_float(r16[1]));
+    const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+    m = mx8_max(__uint_as_float(r32[0]), __uint_as_float(r32[1]));
+    const int byte = mx8_scale_byte(m);
     if (!on) return;
     unsigned char* dst = a.h + row * a.N + col + 4 * lg;
     *reinterpret_cast<unsigned*>(dst) = mx8_pack4(h[0], h[1], h[2], h[3], byte);
@@ -123,7 +125,7 @@ __device__ __forceinline__ TileRef next_tile(TileList& l, const GemmArgs& g, int
     }
 }
 
-// Tile of BM rows by 256 weight rows (gate-up: 128 gate rows and the 128 up rows they meet), eight wavefronts: wavefront (wm, wn)
+// Tile of BM rows by BN = 256 weight rows (gate-up: 128 gate rows and the 128 up rows they meet), eight wavefronts: wavefront (wm, wn)
 // owns 64 weight rows and every second fragment of 16 rows starting at wm.  Fragments without rows are multiplied like the others: the tile's time
 // is that of its loads, and one straight body keeps the accumulators where they are (a body per number of fragments, as alternatives of one
 // switch, had the compiler move and spill them).
@@ -135,24 +137,31 @@ __device__ __forceinline__ TileRef next_tile(TileList& l, const GemmArgs& g, int
 // the loads of weights go out that fill the buffer the stage before has released.  Then the wavefronts meet: everyone's loads of the next stage have landed and nobody reads
 // this one any more.  The second part multiplies the last two fragments from registers, and while it does the weights' fragments are replaced
 // by the next stage's, the next stage's first rows are fetched, and the loads of rows go out into the buffer that has become free.
-template <bool GATE_UP, int BM, int NSX, int NSW> struct Mx8Tile {
-    static constexpr int BN = 256, NW = 8, ROWB = kMxStep;
-    static constexpr int XBYTES = BM * ROWB, WBYTES = BN * ROWB, SBYTES = (BN + BM) * 4;
+template <bool GATE_UP, int BM, int BNN, int NSX, int NSW> struct Mx8Tile {
+    static constexpr int BN = BNN, NW = BN / 32, ROWB = kMxStep;
+    static constexpr int XBYTES = BM * ROWB, WBYTES = BN * ROWB, SBYTES = (BN + (BM + 63) / 64 * 64) * 4;
     static constexpr int XI = XBYTES / (NW * 1024), WI = WBYTES / (NW * 1024);      // 1 KB loads of a wavefront
     static constexpr int MF = BM / 32;                    // fragments of a wavefront
     static constexpr int WBASE = NSX * XBYTES, SBASE = WBASE + NSW * WBYTES, GBASE = SBASE + NSW * SBYTES;
-    static constexpr int LDS = GBASE + 2 * BM * 4;
-    static_assert(LDS <= 160 * 1024 && NSX >= 2 && NSW == 3 && NSX <= NSW, "the rings fit a compute unit");
+    static constexpr int GROWS = (BM + 63) / 64 * 64;     // looked-up rows of a tile
+    static constexpr int LDS = GBASE + 2 * GROWS * 4;
+    static constexpr int WG = NW == 8 ? 1 : 2;            // workgroups of a compute unit
+    static_assert(WG * LDS <= 160 * 1024 && NSX >= 2 && NSW == 3 && NSX <= NSW, "the rings fit a compute unit");
+    static_assert(XBYTES % (NW * 1024) == 0 && (NW == 8 || NW == 4), "whole loads");
+    // scales: the words of 64 rows a load, by wavefronts 0 ..; the weights' by the last ones, all of them in one load where a row group has 256
+    static constexpr int XS = (BM + 63) / 64, WS = NW == 8 ? 1 : 2;
+    static_assert(XS + WS <= NW, "one load of scales a wavefront");
     static constexpr int COLS = GATE_UP ? BN / 2 : BN;    // output columns
 };
 
-template <bool GATE_UP, int BM, int NSX, int NSW>
-__global__ __launch_bounds__(512, 2) void ffn_mx8_kernel(const Mx8Args a) {
-    using C = Mx8Tile<GATE_UP, BM, NSX, NSW>;
+template <bool GATE_UP, int BM, int BN_, int NSX, int NSW>
+__global__ __launch_bounds__(2 * BN_, 2) void ffn_mx8_kernel(const Mx8Args a) {
+    using C = Mx8Tile<GATE_UP, BM, BN_, NSX, NSW>;
     constexpr int XI = C::XI, WI = C::WI, MF = C::MF, BN = C::BN;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int l16 = lane & 15, lg = lane >> 4, wm = wave & 1, wn = wave >> 1;
+    const bool x_scales = wave < C::XS, w_scales = wave >= C::NW - C::WS;
     const unsigned lds0 = lds_addr_of(smem);
     const int nk = (a.K + kMxStep - 1) / kMxStep;
     const bool half = a.K % kMxStep != 0;                  // the last stage of a tile has 64 indices
@@ -174,7 +183,7 @@ __global__ __launch_bounds__(512, 2) void ffn_mx8_kernel(const Mx8Args a) {
     auto piece_of = [&](int ln) { return ((ln & 7) ^ swz(wave * 8 + (ln >> 3))) * 16; };
     const bool upper = piece_of(lane) >= 64;               // absent from a stage of 64 indices: zeros
     const char* const zeros = reinterpret_cast<const char*>(g_mx8_zero_page);
-    long long xinc = kMxStep, winc = kMxStep, sinc = wave < 4 ? (long long)a.E * a.w_rows * 4 : a.x_rows * 4;      // from stage to stage
+    long long xinc = kMxStep, winc = kMxStep, sinc = w_scales ? (long long)a.E * a.w_rows * 4 : a.x_rows * 4;      // from stage to stage
     // Rows of a gathered tile are looked up while the tile before is loaded: their numbers pass through LDS (two tiles' worth), since a wait
     // for a load to a register would wait for every stage in flight.  They are there two stages later: tiles of one or two are too short.
     const bool by_lds = a.gather != nullptr && nk >= 3;
@@ -182,13 +191,13 @@ __global__ __launch_bounds__(512, 2) void ffn_mx8_kernel(const Mx8Args a) {
     auto row_of = [&](const TileRef& t, int r, int tile) {
         const int row = t.row0 + min(r, t.rows - 1);
         if (a.gather == nullptr) return (long long)row;
-        const int slot = by_lds && !prologue ? *reinterpret_cast<const int*>(smem + C::GBASE + ((tile & 1) * BM + min(r, t.rows - 1)) * 4)
+        const int slot = by_lds && !prologue ? *reinterpret_cast<const int*>(smem + C::GBASE + ((tile & 1) * C::GROWS + min(r, t.rows - 1)) * 4)
                                              : a.gather[row];
         return (long long)(slot / a.gather_div);
     };
-    auto weight_of = [&](const TileRef& t, int r) {
+    auto weight_of = [&](const TileRef& t, int r, int n) {         // the first of n neighbours, all inside the matrix
         const int n0 = t.nt * C::COLS;
-        const int c = GATE_UP ? min(n0 + (r & (BN / 2 - 1)), a.N - 1) + (r / (BN / 2)) * a.N : min(n0 + r, a.N - 1);
+        const int c = GATE_UP ? min(n0 + (r & (BN / 2 - 1)), a.N - n) + (r / (BN / 2)) * a.N : min(n0 + r, a.N - n);
         return (long long)t.expert * a.w_rows + c;
     };
     // (in what follows the lane number is made opaque, or what depends on it alone would be kept in registers across the stages)
@@ -229,14 +238,13 @@ __global__ __launch_bounds__(512, 2) void ffn_mx8_kernel(const Mx8Args a) {
 #pragma unroll
         for (int i = 0; i < WV; i++) woff[i] = (unsigned)min(i * C::NW * 8 + r, a.N - 1 - t.nt * C::COLS) * (unsigned)a.K + at;
         wbase = reinterpret_cast<const char*>(a.w) + ((long long)t.expert * a.w_rows + t.nt * C::COLS) * a.K;
-        // scales: one load a wavefront, of 64 weight rows or 64 rows (some of them twice where there are fewer)
-        if (wave < 4) ssrc = reinterpret_cast<const char*>(a.w_scale) + weight_of(t, wave * 64 + ln) * 4;
-        else ssrc = reinterpret_cast<const char*>(a.x_scale) + row_of(t, (wave - 4) % (BM / 64) * 64 + ln, wtile) * 4;
+        if (x_scales) ssrc = reinterpret_cast<const char*>(a.x_scale) + row_of(t, wave * 64 + ln, wtile) * 4;
+        else if (w_scales) ssrc = reinterpret_cast<const char*>(a.w_scale) + (C::WS == 1 ? weight_of(t, ln * 4, 4) : weight_of(t, (wave - C::NW + C::WS) * 64 + ln, 1)) * 4;
         wnext = next_tile(wlist, a.g, ln);
-        if (by_lds && wnext.valid && wave < BM / 64)
-            glds4(a.gather + wnext.row0 + min(wave * 64 + ln, wnext.rows - 1), lds0 + C::GBASE + (((wtile + 1) & 1) * BM + wave * 64) * 4);
+        if (by_lds && wnext.valid && wave < C::XS)
+            glds4(a.gather + wnext.row0 + min(wave * 64 + ln, wnext.rows - 1), lds0 + C::GBASE + (((wtile + 1) & 1) * C::GROWS + wave * 64) * 4);
     };
-    const unsigned sbase = lds0 + C::SBASE + (wave < 4 ? wave * 256 : BN * 4 + (wave - 4) % (BM / 64) * 256);
+    const unsigned sbase = lds0 + C::SBASE + (x_scales ? BN * 4 + wave * 256 : (wave - C::NW + C::WS) * 256);
     auto issue_x = [&](int i) {
         const char* src = half && xkt == nk - 1 && upper ? zeros : xsrc[i];
         glds16(src, lds0 + xdst + (i * C::NW + wave) * 1024);
@@ -249,7 +257,8 @@ __global__ __launch_bounds__(512, 2) void ffn_mx8_kernel(const Mx8Args a) {
             const unsigned at = woff[i % WV] - (half && wkt == nk - 1 && upper ? 64 : 0);
             glds16_s(wbase + (i / WV) * up, at, lds0 + C::WBASE + wdst + (i * C::NW + wave) * 1024);
         } else {
-            glds4(ssrc, sbase + sdst);
+            if (x_scales || (w_scales && C::WS > 1)) glds4(ssrc, sbase + sdst);
+            else if (w_scales) glds16(ssrc, sbase + sdst);
             ssrc += sinc;
             wbase += winc;
         }
@@ -344,7 +353,9 @@ __global__ __launch_bounds__(512, 2) void ffn_mx8_kernel(const Mx8Args a) {
         }
         keep(0, M1);
         // the loads of the next stage have landed: only what was issued behind them may be outstanding
-        wait_vmcnt<NSX == NSW ? XI + WI + 1 : WI + 1>();
+        constexpr int kBehind = NSX == NSW ? XI + WI : WI;
+        if (x_scales || w_scales) wait_vmcnt<kBehind + 1>();
+        else wait_vmcnt<kBehind>();
         lds_barrier();
         xo = xo + C::XBYTES == NSX * C::XBYTES ? 0 : xo + C::XBYTES;
         wo = wo + C::WBYTES == NSW * C::WBYTES ? 0 : wo + C::WBYTES;
@@ -408,9 +419,9 @@ __global__ __launch_bounds__(512, 2) void ffn_mx8_kernel(const Mx8Args a) {
     wait_vmcnt<0>();                                       // no load may land in LDS that is someone else's by then
 }
 
-template <bool GATE_UP, int BM, int NSX, int NSW> hipError_t run_tile(Mx8Args a, hipStream_t st) {
-    using C = Mx8Tile<GATE_UP, BM, NSX, NSW>;
-    auto kern = ffn_mx8_kernel<GATE_UP, BM, NSX, NSW>;
+template <bool GATE_UP, int BM, int BN, int NSX, int NSW> hipError_t run_tile(Mx8Args a, hipStream_t st) {
+    using C = Mx8Tile<GATE_UP, BM, BN, NSX, NSW>;
+    auto kern = ffn_mx8_kernel<GATE_UP, BM, BN, NSX, NSW>;
     static bool attr_set = false;
     if (!attr_set) {
         hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
@@ -419,7 +430,7 @@ template <bool GATE_UP, int BM, int NSX, int NSW> hipError_t run_tile(Mx8Args a,
     }
     a.g.group_m = BM > 128 ? 2 : 1;
     a.g.n_tiles_n = cdiv(a.N, C::COLS);
-    kern<<<max(kNumXcd, num_cus() / kNumXcd * kNumXcd), 512, C::LDS, st>>>(a);
+    kern<<<max(kNumXcd, num_cus() / kNumXcd * kNumXcd) * C::WG, 64 * C::NW, C::LDS, st>>>(a);
     return hipGetLastError();
 }
 
@@ -432,9 +443,9 @@ int tile_bm(const unipool_shape& s) {
 
 template <bool GATE_UP> hipError_t run_mx8(const unipool_shape& s, const Mx8Args& a, hipStream_t st) {
     switch (tile_bm(s)) {
-        case 64: return run_tile<GATE_UP, 64, 3, 3>(a, st);
-        case 128: return run_tile<GATE_UP, 128, 3, 3>(a, st);
-        default: return run_tile<GATE_UP, 192, 2, 3>(a, st);
+        case 64: return run_tile<GATE_UP, 64, 256, 3, 3>(a, st);
+        case 128: return run_tile<GATE_UP, 128, 256, 3, 3>(a, st);
+        default: return run_tile<GATE_UP, 192, 256, 2, 3>(a, st);
     }
 }
 

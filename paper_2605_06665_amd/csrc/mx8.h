@@ -8,6 +8,7 @@
 // step of 128 indices are one word, and the words of neighbouring rows are neighbours.  Bytes past cols are 127.
 #pragma once
 #include "kernels.h"
+#include "route_select.h"
 
 namespace unipool {
 
@@ -18,14 +19,29 @@ constexpr int kMxStep = 128;              // columns of one word of scales
 constexpr int kMxBias = 127;
 constexpr int kMxNan = 255;               // scale byte of a block that holds a NaN or an infinity
 
-// Magnitudes as integers: they order as the floats do, with infinity and NaN on top (fmaxf would drop a NaN).
-__device__ __forceinline__ unsigned mx8_mag(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+// Larger magnitude of two values; NaN if one of them is (fmaxf would drop it).  Chains of it become v_maximum3_f32 with |.| on its operands.
+__device__ __forceinline__ float mx8_max(float a, float b) { return __builtin_elementwise_maximum(__builtin_fabsf(a), __builtin_fabsf(b)); }
 
-// Scale byte of a block from the largest magnitude: amax = 2^(E - 127) (1 + m / 2^23) and 448 = 2^8 * 1.75, so e = E - 135, one more
-// if the fraction is over 0.75.
-__device__ __forceinline__ int mx8_scale_byte(unsigned amax) {
-    if (amax >= 0x7f800000u) return kMxNan;
-    const int e = (int)(amax >> 23) - 135 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
+// Largest magnitude over LPB neighbouring lanes, the same in all of them (every lane of the wavefront is active).
+template <int LPB> __device__ __forceinline__ float mx8_lanes_max(float v) {
+    static_assert(LPB == 4 || LPB == 8 || LPB == 32, "8, 4 or 1 values a lane");
+    v = mx8_max(v, dpp_f<kDppQuadXor1>(v));
+    v = mx8_max(v, dpp_f<kDppQuadXor2>(v));
+    if constexpr (LPB >= 8) v = mx8_max(v, dpp_f<kDppRowHalfMirror>(v));
+    if constexpr (LPB == 32) {
+        v = mx8_max(v, dpp_f<kDppRowMirror>(v));
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = mx8_max(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    return v;
+}
+
+// Scale byte of a block from its largest magnitude: amax = 2^(E - 127) (1 + m / 2^23) and 448 = 2^8 * 1.75, so e = E - 135, one more if
+// the fraction is over 0.75.
+__device__ __forceinline__ int mx8_scale_byte(float amax) {
+    const unsigned b = __float_as_uint(amax) & 0x7fffffffu;
+    if (b >= 0x7f800000u) return kMxNan;
+    const int e = (int)(b >> 23) - 135 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
     return max(e, -127) + kMxBias;
 }
 // 2^-e, exact: e lies between -127 and 120

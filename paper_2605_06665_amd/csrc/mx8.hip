@@ -37,11 +37,10 @@ __global__ __launch_bounds__(256) void quantize_mx8_kernel(const TA* __restrict_
 #pragma unroll
             for (int i = 0; i < 8; i++) v[i] = 0.f;
         }
-        unsigned m = 0;
+        float m = v[0];
 #pragma unroll
-        for (int i = 0; i < 8; i++) m = max(m, mx8_mag(v[i]));
-        m = max(m, (unsigned)__shfl_xor((int)m, 1, 64));
-        m = max(m, (unsigned)__shfl_xor((int)m, 2, 64));
+        for (int i = 1; i < 8; i++) m = mx8_max(m, v[i]);
+        m = mx8_lanes_max<4>(m);
         const int byte = col < cols ? mx8_scale_byte(m) : kMxBias;
         if (on) {
             const unsigned lo = mx8_pack4(v[0], v[1], v[2], v[3], byte), hi = mx8_pack4(v[4], v[5], v[6], v[7], byte);

@@ -52,11 +52,10 @@ template <int N>
 __device__ __forceinline__ void store_mx8(const float (&y)[N], bool on, size_t rows, size_t row, int d, int col, unsigned char* q,
                                           unsigned char* scale) {
     constexpr int LPB = kMxBlock / N;
-    unsigned m = 0;
+    float m = y[0];
 #pragma unroll
-    for (int i = 0; i < N; i++) m = max(m, mx8_mag(y[i]));
-#pragma unroll
-    for (int o = 1; o < LPB; o <<= 1) m = max(m, (unsigned)__shfl_xor((int)m, o, 64));
+    for (int i = 1; i < N; i++) m = mx8_max(m, y[i]);
+    m = mx8_lanes_max<LPB>(m);
     if (!on) return;
     const int byte = mx8_scale_byte(m);
     unsigned char* dst = q + row * d + col;
@@ -99,7 +98,10 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rmsnorm_kernel(const No
     TA* y = a.y ? (TA*)a.y + o : nullptr;
     constexpr int STEP = 64 * W * N;
     float v[R][N];
+    P wp[R];                                               // requested with the row, or a second latency would follow the sum
     float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < R; i++) wp[i] = i * STEP + lane * N < d ? *reinterpret_cast<const P*>(w + i * STEP + lane * N) : P{};
     auto fetch = [&](int col, float (&s)[N]) {
 #pragma unroll
         for (int i = 0; i < N; i++) s[i] = 0.f;
@@ -113,13 +115,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rmsnorm_kernel(const No
             }
         }
     };
-    auto finish = [&](int col, const float (&s)[N], float rs) {
+    auto finish = [&](int col, const float (&s)[N], const P& wv, float rs) {
         const bool on = col < d;
         float out[N];
-        if (on) {
-            unpack<TA, N>(*reinterpret_cast<const P*>(w + col), out);
-            if (h != nullptr) *reinterpret_cast<P*>(h + col) = pack<TA, N>(s);
-        }
+        unpack<TA, N>(wv, out);
+        if (on && h != nullptr) *reinterpret_cast<P*>(h + col) = pack<TA, N>(s);
 #pragma unroll
         for (int i = 0; i < N; i++) out[i] = on ? s[i] * rs * out[i] : 0.f;
         if (on && y != nullptr) *reinterpret_cast<P*>(y + col) = pack<TA, N>(out);
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rmsnorm_kernel(const No
     ss = row_sum<W>(ss, red);
     const float rs = 1.0f / sqrtf(ss / (float)d + a.eps);
 #pragma unroll
-    for (int i = 0; i < R; i++) finish(i * STEP + lane * N, v[i], rs);
+    for (int i = 0; i < R; i++) finish(i * STEP + lane * N, v[i], wp[i], rs);
     if (a.q != nullptr) {
         const int b = d / kMxBlock + lane;                  // blocks that fill the last word of scales
         if (b < cdiv(d, kMxStep) * 4) a.scale[mx8_scale_at(a.T, row, b)] = kMxBias;
@@ -149,12 +149,13 @@ struct NormBwdArgs {
     float eps;
 };
 
-// As above; a workgroup takes the rows blockIdx.x, blockIdx.x + gridDim.x, ... (W == 1: four at a time) and holds its share of
+// As above; a workgroup takes the rows blockIdx.x, blockIdx.x + gridDim.x, ... (W == 1: eight at a time) and holds its share of
 // d_weight in registers.
+constexpr int kBwdRows = 8;
 template <typename TA, int N, int W, int R>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rmsnorm_bwd_kernel(const NormBwdArgs a) {
+__global__ __launch_bounds__(W == 1 ? 64 * kBwdRows : 64 * W) void rmsnorm_bwd_kernel(const NormBwdArgs a) {
     typedef typename Pack<TA, N>::type P;
-    constexpr int kRows = W == 1 ? 4 : 1;
+    constexpr int kRows = W == 1 ? kBwdRows : 1;
     constexpr int STEP = 64 * W * N;
     __shared__ float red[2][W];
     __shared__ float sums[W == 1 ? STEP * R : 1];
@@ -220,8 +221,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rmsnorm_bwd_kernel(cons
     }
     float* part = a.part + (size_t)blockIdx.x * d;
     if constexpr (W == 1) {
-        // the four wavefronts one after the other, so that the sum has one order
-        for (int v = 0; v < 4; v++) {
+        // the wavefronts one after the other, so that the sum has one order
+        for (int v = 0; v < kBwdRows; v++) {
             if (wave == v) {
 #pragma unroll
                 for (int i = 0; i < R; i++)
@@ -233,7 +234,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rmsnorm_bwd_kernel(cons
             }
             __syncthreads();
         }
-        for (int c = threadIdx.x; c < d; c += 256) part[c] = sums[c / STEP * STEP + (c % N) * 64 + c % STEP / N];
+        for (int c = threadIdx.x; c < d; c += 64 * kBwdRows) part[c] = sums[c / STEP * STEP + (c % N) * 64 + c % STEP / N];
     } else {
 #pragma unroll
         for (int i = 0; i < R; i++)
@@ -322,9 +323,9 @@ hipError_t run_norm_bwd(NormBwdArgs a, float* d_weight, float* part, hipStream_t
     const bool wide = a.d % n == 0 && aligned16({a.h, a.weight, a.dy, a.dh, a.dx});
     int grid = 1;
     with_norm_form<TA>(a.d, wide, [&](auto nn, auto w, auto r) {
-        grid = std::min(kNormParts, w() == 1 ? cdiv(a.T, 4) : a.T);
+        grid = std::min(kNormParts, w() == 1 ? cdiv(a.T, kBwdRows) : a.T);
         a.part = grid == 1 ? d_weight : part;
-        rmsnorm_bwd_kernel<TA, nn(), w(), r()><<<grid, w() == 1 ? 256 : 64 * w(), 0, st>>>(a);
+        rmsnorm_bwd_kernel<TA, nn(), w(), r()><<<grid, w() == 1 ? 64 * kBwdRows : 64 * w(), 0, st>>>(a);
     });
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || grid == 1) return e;

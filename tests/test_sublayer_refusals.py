@@ -107,7 +107,7 @@ def test_experts(U):
             call(**{n: P + 8})
     for n in ("x_scale", "w_gate_up_scale", "w_down_scale", "h_scale"):
         with pytest.raises(U.UniPoolError, match="aligned to 4"):
-            call(**{n: P + 2})
+            call(**{n: P + (8 if n[0] == "w" else 2)})
     with pytest.raises(U.UniPoolError, match="bfloat16 mode only"):
         call(sh=shape(U, dtype=U.F32))
     with pytest.raises(U.UniPoolError, match="multiples of 64"):
