@@ -90,14 +90,17 @@ __device__ __forceinline__ int few_experts(const int32_t* offsets, int E, int* l
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int n_list = 0;
+    // all offsets are requested together: one latency instead of one per pass
+    int first[kMaxE / kThreads], rows[kMaxE / kThreads];
 #pragma unroll
     for (int p = 0; p < kMaxE / kThreads; p++) {
         const int e = p * kThreads + tid;
-        int r0 = 0, n = 0;
-        if (e < E) {
-            r0 = offsets[e];
-            n = offsets[e + 1] - r0;
-        }
+        first[p] = e < E ? offsets[e] : 0;
+        rows[p] = e < E ? offsets[e + 1] - first[p] : 0;
+    }
+#pragma unroll
+    for (int p = 0; p < kMaxE / kThreads; p++) {
+        const int e = p * kThreads + tid, r0 = first[p], n = rows[p];
         const unsigned long long has = __ballot(n > 0);
         if (lane == 0) wcnt[p][wave] = __popcll(has);
         __syncthreads();

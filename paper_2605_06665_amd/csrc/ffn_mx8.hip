@@ -21,7 +21,7 @@ namespace {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 struct Mx8Args {
-    GemmArgs g;                      // tile list only (tile_meta, n_tiles_n, group_m)
+    GemmArgs g;                      // tile list only (n_tiles_n, group_m)
     const unsigned char* x;          // [rows][K], or the tokens when gather is given
     const unsigned char* x_scale;    // [ceil(K / 128)][x_rows][4]
     long long x_rows;
@@ -82,14 +82,53 @@ __device__ __forceinline__ void glds4(const void* gptr, unsigned lds_addr) {
                  : "memory", "m0");
 }
 
-// The tiles of a workgroup in the order of TileWalk, 64 at a time: lane i holds the tile of round base + i, so the divisions and the table
-// reads of a tile are done once for 64 of them.
+// The tile list.  The rows of an expert are cut into equal tiles of at most BM rows (multiples of 16); with BM > 128 an expert takes an
+// even number of places, since the two row tiles of a pair run side by side and share their weights through L2.  Every workgroup
+// counts the places for itself (place[e]: those of the experts before e), which takes a fraction of a launch.
+__device__ __forceinline__ int row_tiles_of(int rows, int bm) {
+    const int n = (rows + bm - 1) / bm;
+    return bm > 128 ? (n + 1) & ~1 : n;
+}
+__device__ __forceinline__ void count_places(const int32_t* offsets, int E, int bm, int* place) {
+    constexpr int PER = kMaxE / 64;
+    if (threadIdx.x < 64) {
+        int n[PER], sum = 0;
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            const int e = threadIdx.x * PER + i;
+            n[i] = e < E ? offsets[e + 1] - offsets[e] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            n[i] = row_tiles_of(n[i], bm);
+            sum += n[i];
+        }
+        int upto = sum;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(upto, d, 64);
+            if ((int)threadIdx.x >= d) upto += o;
+        }
+        int at = upto - sum;
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            place[threadIdx.x * PER + i] = at;
+            at += n[i];
+        }
+        if (threadIdx.x == 63) place[kMaxE] = at;
+    }
+    __syncthreads();
+}
+
+// The tiles of a workgroup in the order of TileWalk, 64 at a time: lane i holds the tile of round base + i, so the divisions and the
+// search of a tile are done once for 64 of them.
 struct TileList {
     int next, base;                  // round that comes next; round of lane 0
     int rows, expert, row0, nt;      // per lane; rows: 0 a place without a tile, -1 past the end
 };
-__device__ __forceinline__ void tiles_at(TileList& l, const GemmArgs& g, int round0, int lane) {
-    const int n_mt = g.tile_meta[0], G = g.group_m, per_group = G * g.n_tiles_n;
+__device__ __forceinline__ void tiles_at(TileList& l, const Mx8Args& a, const int* place, int bm, int round0, int lane) {
+    const GemmArgs& g = a.g;
+    const int n_mt = place[kMaxE], G = g.group_m, per_group = G * g.n_tiles_n;
     const int total = ((n_mt + G - 1) / G) * per_group, per_xcd = (total + kNumXcd - 1) / kNumXcd;
     const int xcd = blockIdx.x % kNumXcd, slot = blockIdx.x / kNumXcd, P = gridDim.x / kNumXcd;
     const int round = round0 + lane, lt = xcd * per_xcd + round * P + (slot + round) % P;
@@ -101,16 +140,21 @@ __device__ __forceinline__ void tiles_at(TileList& l, const GemmArgs& g, int rou
     }
     const int rem = lt % per_group, mt = lt / per_group * G + rem % G;
     if (mt >= n_mt) return;
-    const int4 m = *reinterpret_cast<const int4*>(g.tile_meta + kTileBase + 4 * mt);
-    l.expert = m.x;
-    l.row0 = m.y;
-    l.rows = max(m.z, 0);
+    int e = 0;                       // the last expert whose first place is not behind mt
+#pragma unroll
+    for (int step = kMaxE / 2; step > 0; step >>= 1)
+        if (place[e + step] <= mt) e += step;
+    const int r0 = a.offsets[e], rows = a.offsets[e + 1] - r0;
+    const int n = (rows + bm - 1) / bm, per = ((rows + n - 1) / n + 15) / 16 * 16, i = mt - place[e];
+    l.expert = e;
+    l.row0 = r0 + i * per;
+    l.rows = max(0, min(per, rows - i * per));
     l.nt = rem / G;
 }
-__device__ __forceinline__ TileRef next_tile(TileList& l, const GemmArgs& g, int lane) {
+__device__ __forceinline__ TileRef next_tile(TileList& l, const Mx8Args& a, const int* place, int bm, int lane) {
     TileRef t = {0, 0, 0, 0, 0, -1};
     for (;;) {
-        if (l.next - l.base == 64) tiles_at(l, g, l.next, lane);
+        if (l.next - l.base == 64) tiles_at(l, a, place, bm, l.next, lane);
         const int i = l.next - l.base;
         const int rows = __builtin_amdgcn_readlane(l.rows, i);
         if (rows < 0) return t;
@@ -144,7 +188,8 @@ template <bool GATE_UP, int BM, int BNN, int NSX, int NSW> struct Mx8Tile {
     static constexpr int MF = BM / 32;                    // fragments of a wavefront
     static constexpr int WBASE = NSX * XBYTES, SBASE = WBASE + NSW * WBYTES, GBASE = SBASE + NSW * SBYTES;
     static constexpr int GROWS = (BM + 63) / 64 * 64;     // looked-up rows of a tile
-    static constexpr int LDS = GBASE + 2 * GROWS * 4;
+    static constexpr int PBASE = GBASE + 2 * GROWS * 4;
+    static constexpr int LDS = PBASE + (kMaxE + 1) * 4;
     static constexpr int WG = NW == 8 ? 1 : 2;            // workgroups of a compute unit
     static_assert(WG * LDS <= 160 * 1024 && NSX >= 2 && NSW == 3 && NSX <= NSW, "the rings fit a compute unit");
     static_assert(XBYTES % (NW * 1024) == 0 && (NW == 8 || NW == 4), "whole loads");
@@ -169,8 +214,10 @@ __global__ __launch_bounds__(2 * BN_, 2) void ffn_mx8_kernel(const Mx8Args a) {
     auto swz = [](int row) { return (row >> 1) & 7; };
 
     // ---- load cursors ---------------------------------------------------------------------------------------
+    int* const place = reinterpret_cast<int*>(smem + C::PBASE);
+    count_places(a.offsets, a.E, BM, place);
     TileList xlist, wlist;
-    tiles_at(xlist, a.g, 0, lane);
+    tiles_at(xlist, a, place, BM, 0, lane);
     wlist = xlist;
     TileList clist = xlist;
     bool xon, won;
@@ -204,7 +251,7 @@ __global__ __launch_bounds__(2 * BN_, 2) void ffn_mx8_kernel(const Mx8Args a) {
     auto next_x = [&]() {
         int ln = lane;
         asm volatile("" : "+v"(ln));
-        const TileRef t = next_tile(xlist, a.g, ln);
+        const TileRef t = next_tile(xlist, a, place, BM, ln);
         xon = t.valid;
         xkt = 0;
         xtile++;
@@ -218,7 +265,7 @@ __global__ __launch_bounds__(2 * BN_, 2) void ffn_mx8_kernel(const Mx8Args a) {
 #pragma unroll
         for (int i = 0; i < XI; i++) xsrc[i] = reinterpret_cast<const char*>(a.x) + row_of(t, i * C::NW * 8 + r, xtile) * a.K + at;
     };
-    TileRef wnext = next_tile(wlist, a.g, lane);
+    TileRef wnext = next_tile(wlist, a, place, BM, lane);
     if (!wnext.valid) return;                              // no tile for this workgroup
     auto next_w = [&]() {
         int ln = lane;
@@ -240,7 +287,7 @@ __global__ __launch_bounds__(2 * BN_, 2) void ffn_mx8_kernel(const Mx8Args a) {
         wbase = reinterpret_cast<const char*>(a.w) + ((long long)t.expert * a.w_rows + t.nt * C::COLS) * a.K;
         if (x_scales) ssrc = reinterpret_cast<const char*>(a.x_scale) + row_of(t, wave * 64 + ln, wtile) * 4;
         else if (w_scales) ssrc = reinterpret_cast<const char*>(a.w_scale) + (C::WS == 1 ? weight_of(t, ln * 4, 4) : weight_of(t, (wave - C::NW + C::WS) * 64 + ln, 1)) * 4;
-        wnext = next_tile(wlist, a.g, ln);
+        wnext = next_tile(wlist, a, place, BM, ln);
         if (by_lds && wnext.valid && wave < C::XS)
             glds4(a.gather + wnext.row0 + min(wave * 64 + ln, wnext.rows - 1), lds0 + C::GBASE + (((wtile + 1) & 1) * C::GROWS + wave * 64) * 4);
     };
@@ -383,7 +430,7 @@ __global__ __launch_bounds__(2 * BN_, 2) void ffn_mx8_kernel(const Mx8Args a) {
     for (;;) {
         int ln = lane;
         asm volatile("" : "+v"(ln));
-        const TileRef t = next_tile(clist, a.g, ln);
+        const TileRef t = next_tile(clist, a, place, BM, ln);
         if (!t.valid) break;
         const int col = t.nt * C::COLS + wn * (GATE_UP ? 32 : 64);       // the wavefront's columns are inside N or outside as a whole
         const int mi = col < a.N ? (((t.rows + 15) >> 4) - wm + 1) >> 1 : 0;
@@ -434,17 +481,36 @@ template <bool GATE_UP, int BM, int BN, int NSX, int NSW> hipError_t run_tile(Mx
     return hipGetLastError();
 }
 
-// Rows of a tile: one tile for most experts where that is possible.
-int tile_bm(const unipool_shape& s) {
-    const double S = (double)s.T * s.k, used = s.E * -std::expm1(-S / s.E), r = S / used;       // rows of an expert that has any
-    const double most = r + 2.0 * std::sqrt(r);
-    return most <= 64 ? 64 : most <= 128 ? 128 : 192;
+// Which form a call takes, from the rows r of an expert that has any (as if the picks were independent) and from how many rounds its
+// gate-up tiles of 128 rows by 256 weight rows are on the card's compute units.  All of the call, us, three sets of weights in turn:
+//   few: up to 64 tokens, with few tasks (64 experts of 768 x 2048, k = 2, 1 token: few 16.9, tiles of 64 x 128 22.2, 4 tokens 20.6 / 23.5; but 5
+//     tokens of 90 experts of 832 x 1472, k = 3 29.1 / 24.9), or where the reductions are long (192 experts of 1536 x 4096, k = 2, 4 tokens 44 / 52,
+//     64 tokens 344 / 359; but 40 tokens of the 90 experts 76 / 68);
+//   128 weight rows, two workgroups to a compute unit, while there are less than 16 rounds of the wide ones, or 4 with more than 96
+//     rows (64 x 128 / 96 x 128 / 64 x 256 / 128 x 256: 90 experts, 50 rows, hot 106 / 110 / 117 / 114; 16 experts of 768 x 2048, 37 rows 28.5 /
+//     29.2 / 31.8 / 35.8, 187 rows 50 / 45 / 51 / 47);
+//   256 weight rows beyond (192 experts of 1536 x 4096, 11 rows 719 / 726 / 651 / 670, 42 rows 761 / 759 / 717 / 728, 85 rows 1087 / 913 / 1004 / 789);
+//   192 rows where experts take several tiles of 128 (the 192 experts, 125 rows: 128 x 256 961, 192 x 256 866; 512 of 1024 x 704, 256 rows 574 / 560).
+enum Mx8Form { MX8_FEW, MX8_64x128, MX8_96x128, MX8_64x256, MX8_128x256, MX8_192x256 };
+Mx8Form mx8_form(const unipool_shape& s) {
+    const double S = (double)s.T * s.k, used = s.E * -std::expm1(-S / s.E), r = S / used, most = r + 2.0 * std::sqrt(r);
+    const int cus = num_cus();
+    if (s.T <= 16 || (s.T <= 64 && S <= 8.0 * s.E)) {
+        const double tasks = std::min(S, (double)s.E) * (s.d_ff / 32);
+        if (tasks <= 2.0 * cus || std::min(s.d_model, s.d_ff) >= 1536) return MX8_FEW;
+    }
+    const double rounds = used * std::ceil((r + std::sqrt(r)) / 128) * cdiv(s.d_ff, 128) / cus;
+    if (r > 96) return rounds < 4 ? MX8_96x128 : most <= 128 ? MX8_128x256 : MX8_192x256;
+    if (rounds < 16) return most <= 64 ? MX8_64x128 : MX8_96x128;
+    return most <= 32 ? MX8_64x256 : MX8_128x256;
 }
 
-template <bool GATE_UP> hipError_t run_mx8(const unipool_shape& s, const Mx8Args& a, hipStream_t st) {
-    switch (tile_bm(s)) {
-        case 64: return run_tile<GATE_UP, 64, 256, 3, 3>(a, st);
-        case 128: return run_tile<GATE_UP, 128, 256, 3, 3>(a, st);
+template <bool GATE_UP> hipError_t run_mx8(Mx8Form form, const Mx8Args& a, hipStream_t st) {
+    switch (form) {
+        case MX8_64x128: return run_tile<GATE_UP, 64, 128, 3, 3>(a, st);
+        case MX8_96x128: return run_tile<GATE_UP, 96, 128, 2, 3>(a, st);
+        case MX8_64x256: return run_tile<GATE_UP, 64, 256, 3, 3>(a, st);
+        case MX8_128x256: return run_tile<GATE_UP, 128, 256, 3, 3>(a, st);
         default: return run_tile<GATE_UP, 192, 256, 2, 3>(a, st);
     }
 }
@@ -471,12 +537,11 @@ __device__ __forceinline__ void few_mx8_task(const Mx8Args& a, int e, int c0, in
     const bool half = a.K % kMxStep != 0;                  // the last step has 64 indices
     // addresses are a wave-uniform base and a 32-bit offset per lane (at most 512 rows, and 16 rows of weights)
     unsigned xo[R], xso[R];
+    int row[R];
 #pragma unroll
     for (int r = 0; r < R; r++) {
-        int row = row0 + min(16 * r + l16, rows - 1);
-        if (a.gather != nullptr) row = a.gather[row] / a.gather_div;
-        xo[r] = (unsigned)row * (unsigned)a.K + 16 * lg;
-        xso[r] = (unsigned)row * 4 + lg;
+        row[r] = row0 + min(16 * r + l16, rows - 1);
+        if (a.gather != nullptr) row[r] = a.gather[row[r]];
     }
     const unsigned wo = (unsigned)(lane & 7) * (unsigned)a.K + 16 * chunk, wso = l16 * 4 + lg;
     // in a half step the pieces past the end are read from the first half: any finite value will do beside rows of zeros
@@ -494,11 +559,10 @@ __device__ __forceinline__ void few_mx8_task(const Mx8Args& a, int e, int c0, in
         for (int f = 0; f < NF; f++) acc[r][f] = f32x4{0.f, 0.f, 0.f, 0.f};
     // wave-uniform addresses of the step that is requested next; past the end it stays the last one, whose values are never used
     const unsigned char *wk = we, *wsk = wse, *xk = a.x, *xsk = a.x_scale;
-    int next = 0;
-    auto fetch = [&](int u) {
-        const bool last = next == nk - 1;
-        const bool cut = half && last;
-        unsigned o = cut ? wo_cut : wo, so = wso;
+    int next_w = 0, next_x = 0;
+    auto fetch_w = [&](int u) {
+        const bool last = next_w == nk - 1;
+        unsigned o = half && last ? wo_cut : wo, so = wso;
         // (known to the compiler as 32-bit offsets right here: widened outside the loop they would be added to every base in vector registers)
         asm volatile("" : "+v"(o), "+v"(so));
 #pragma unroll
@@ -509,18 +573,22 @@ __device__ __forceinline__ void few_mx8_task(const Mx8Args& a, int e, int c0, in
                 wq[u][f][h] = __builtin_nontemporal_load(reinterpret_cast<const u32x4v*>(wk + (fr + h * 8) * a.K + o));
             ws[u][f] = (wsk + fr * 4)[so];
         }
+        next_w += last ? 0 : 1;
+        wk += last ? 0 : kMxStep;
+        wsk += last ? 0 : w_plane;
+    };
+    auto fetch_x = [&](int u) {
+        const bool last = next_x == nk - 1;
 #pragma unroll
         for (int r = 0; r < R; r++) {
             unsigned q = xo[r], p = xso[r];
             asm volatile("" : "+v"(q), "+v"(p));
             xq[u][r][0] = *reinterpret_cast<const u32x4v*>(xk + q);
-            xq[u][r][1] = *reinterpret_cast<const u32x4v*>(xk + (cut ? 0 : 64) + q);
+            xq[u][r][1] = *reinterpret_cast<const u32x4v*>(xk + (half && last ? 0 : 64) + q);
             xs[u][r] = xsk[p];
         }
-        next += last ? 0 : 1;
-        wk += last ? 0 : kMxStep;
+        next_x += last ? 0 : 1;
         xk += last ? 0 : kMxStep;
-        wsk += last ? 0 : w_plane;
         xsk += last ? 0 : x_plane;
     };
     // last: a half step's second half counts as zeros, with scales that are not NaN
@@ -543,14 +611,25 @@ __device__ __forceinline__ void few_mx8_task(const Mx8Args& a, int e, int c0, in
                                                                             ws[u][f], 0, xs[u][r]);
         }
     };
+    // the weights first: which rows meet them is still being looked up
 #pragma unroll
-    for (int u = 0; u < D; u++) fetch(u);
+    for (int u = 0; u < D; u++) fetch_w(u);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int r = 0; r < R; r++) {
+        if (a.gather != nullptr) row[r] /= a.gather_div;
+        xo[r] = (unsigned)row[r] * (unsigned)a.K + 16 * lg;
+        xso[r] = (unsigned)row[r] * 4 + lg;
+    }
+#pragma unroll
+    for (int u = 0; u < D; u++) fetch_x(u);
     int s = 0;
     for (; s + D < nk; s += D) {
 #pragma unroll
         for (int u = 0; u < D; u++) {
             multiply(u, false);
-            fetch(u);
+            fetch_w(u);
+            fetch_x(u);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -615,19 +694,15 @@ template <bool GATE_UP> hipError_t run_few_mx8(const unipool_shape& s, const Mx8
     return hipGetLastError();
 }
 
-bool few_mx8(const unipool_shape& s) { return s.T <= 16 || (s.T <= 64 && s.T * s.k <= 8 * s.E); }
-
 }  // namespace
 
 hipError_t mx8_ffn_fwd(const unipool_shape& s, const void* x, const void* x_scale, const int32_t* slot_of_row, const int32_t* offsets,
                        const void* wgu, const void* wgu_scale, const void* wd, const void* wd_scale, void* h, void* h_scale, void* y,
-                       int32_t* tile_meta, hipStream_t st) {
-    const bool few = few_mx8(s);
-    hipError_t e = few ? hipSuccess : mfma_build_tiles(s, offsets, tile_bm(s), tile_meta, st);
-    if (e != hipSuccess) return e;
+                       hipStream_t st) {
+    const Mx8Form form = mx8_form(s);
+    const bool few = form == MX8_FEW;
     const long long S = (long long)s.T * s.k;
     Mx8Args a = {};
-    a.g.tile_meta = tile_meta;
     a.offsets = offsets;
     a.x = (const unsigned char*)x; a.x_scale = (const unsigned char*)x_scale;
     a.x_rows = slot_of_row ? s.T : S;
@@ -636,10 +711,9 @@ hipError_t mx8_ffn_fwd(const unipool_shape& s, const void* x, const void* x_scal
     a.w_rows = 2 * s.d_ff; a.E = s.E;
     a.K = s.d_model; a.N = s.d_ff;
     a.h = (unsigned char*)h; a.h_scale = (unsigned char*)h_scale; a.S = S;
-    e = few ? run_few_mx8<true>(s, a, st) : run_mx8<true>(s, a, st);
+    hipError_t e = few ? run_few_mx8<true>(s, a, st) : run_mx8<true>(form, a, st);
     if (e != hipSuccess) return e;
     Mx8Args b = {};
-    b.g.tile_meta = tile_meta;
     b.offsets = offsets;
     b.x = (const unsigned char*)h; b.x_scale = (const unsigned char*)h_scale;
     b.x_rows = S;
@@ -647,7 +721,7 @@ hipError_t mx8_ffn_fwd(const unipool_shape& s, const void* x, const void* x_scal
     b.w_rows = s.d_model; b.E = s.E;
     b.K = s.d_ff; b.N = s.d_model;
     b.y = (bf16*)y; b.S = S;
-    return few ? run_few_mx8<false>(s, b, st) : run_mx8<false>(s, b, st);
+    return few ? run_few_mx8<false>(s, b, st) : run_mx8<false>(form, b, st);
 }
 
 }  // namespace unipool

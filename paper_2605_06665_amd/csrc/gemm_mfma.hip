@@ -1251,15 +1251,6 @@ int num_cus() {
     return n;
 }
 
-// Table of tiles of bm rows (a multiple of 16, at most 128 or 256) for the row-grouped products of another file.
-hipError_t mfma_build_tiles(const unipool_shape& s, const int32_t* offsets, int bm, int32_t* meta, hipStream_t st) {
-    TileTables t = {};
-    t.meta[0] = meta; t.bm[0] = bm;
-    t.pair_cnt = pair_counters(meta, s.E, s.T * s.k);
-    build_tiles_kernel<<<1, 512, 0, st>>>(offsets, s.E, t);
-    return hipGetLastError();
-}
-
 bool mfma_ffn_supported(const unipool_shape& s) {
     // the tile table is built by one workgroup with a thread per expert; the weight-gradient kernel
     // keeps the per-layer row ranges of an expert in LDS

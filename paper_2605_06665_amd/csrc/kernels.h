@@ -108,7 +108,6 @@ hipError_t few_ffn_fwd(const unipool_shape& s, const void* x, const int32_t* off
                        void* a_out, void* b_out, void* h_out, void* y, hipStream_t st,
                        const int32_t* slot_of_row = nullptr);
 
-hipError_t mfma_build_tiles(const unipool_shape& s, const int32_t* offsets, int bm, int32_t* meta, hipStream_t st);
 
 // ---- norm.hip ---------------------------------------------------------------------
 hipError_t launch_rmsnorm(const unipool_shape& s, const void* x, const void* residual, const void* weight, float eps, void* h,
@@ -121,7 +120,7 @@ hipError_t launch_rmsnorm_bwd(const unipool_shape& s, const void* h, const void*
 hipError_t launch_quantize_mx8(int dtype, const void* src, long long rows, int cols, void* q, void* scale, hipStream_t st);
 hipError_t mx8_ffn_fwd(const unipool_shape& s, const void* x, const void* x_scale, const int32_t* slot_of_row, const int32_t* offsets,
                        const void* wgu, const void* wgu_scale, const void* wd, const void* wd_scale, void* h, void* h_scale, void* y,
-                       int32_t* tile_meta, hipStream_t st);
+                       hipStream_t st);
 
 // ---- balance.hip -------------------------------------------------------------------
 // cnt_part and loss_part: the areas of the router's partial counts and score sums; state: two words
