@@ -375,6 +375,12 @@ int unipool_expert_ffn_fwd_mx8(const unipool_shape* shape, const void* x_q, cons
                                void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Which form unipool_expert_ffn_fwd_mx8 takes at a shape, for tests and measurements: 0 streams the weights to registers, otherwise
+ * its tiles as 1000 * rows + weight rows.  The form changes no bit of a row's result.  Negative on an invalid shape.
+ */
+int unipool_mx8_form(const unipool_shape* shape);
+
+/*
  * Monte-Carlo estimate of the NormRouter calibration constant c (App. H (NormRouter Monte Carlo initialization), Alg. 1) from draws
  * the caller supplies: for every row x of samples, y = relu(x / ||x||_2), the k largest
  * components of y, 1 / their 2-norm; c is the mean over the rows.  A row without a positive

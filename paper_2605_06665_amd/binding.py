@@ -33,7 +33,7 @@ ENTRY_POINTS = ("unipool_workspace_bytes", "unipool_last_error", "unipool_versio
                 "unipool_expert_ffn_recompute", "unipool_expert_ffn_bwd", "unipool_expert_wgrad", "unipool_combine",
                 "unipool_combine_bwd", "unipool_pool_aux_loss", "unipool_estimate_c",
                 "unipool_distinct_experts", "unipool_route_bwd_add", "unipool_seq_balance_loss", "unipool_rmsnorm", "unipool_rmsnorm_bwd",
-                "unipool_quantize_mx8", "unipool_expert_ffn_fwd_mx8")
+                "unipool_quantize_mx8", "unipool_expert_ffn_fwd_mx8", "unipool_mx8_form")
 
 
 def lib_path() -> str:
@@ -61,6 +61,8 @@ def load_library():
         lib.unipool_fast_path.argtypes = [SP]
         lib.unipool_tile_forms.restype = I
         lib.unipool_tile_forms.argtypes = [SP, I, I]
+        lib.unipool_mx8_form.restype = I
+        lib.unipool_mx8_form.argtypes = [SP]
         sigs = {
             "unipool_route": [SP] + [P] * 7 + [P, Z, P],
             "unipool_route_bwd": [SP] + [P] * 9 + [I, P, Z, P],
@@ -336,6 +338,13 @@ def quantize_mx8(dtype, rows, cols, src, q, scale, stream=None):
     """src [rows, cols] (dtype F32 or BF16) to e4m3 bytes q [rows, cols] and scales of mx8_scale_shape(rows, cols), both uint8."""
     _check((_LIB or load_library()).unipool_quantize_mx8(dtype, rows, cols, *_ptrs(src, q, scale), _stream(stream)),
            "unipool_quantize_mx8")
+
+
+def mx8_form(shape: Shape) -> int:
+    """Form of expert_ffn_fwd_mx8: 0 weights streamed to registers, else tiles as 1000 * rows + weight rows."""
+    rc = load_library().unipool_mx8_form(ctypes.byref(shape))
+    _check(rc if rc < 0 else 0, "unipool_mx8_form")
+    return rc
 
 
 def expert_ffn_fwd_mx8(shape, x_q, x_scale, slot_of_row, expert_offsets, w_gate_up_q, w_gate_up_scale, w_down_q, w_down_scale,

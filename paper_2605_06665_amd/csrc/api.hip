@@ -517,6 +517,13 @@ int unipool_quantize_mx8(int dtype, long long rows, int cols, const void* src, v
     return check_hip(launch_quantize_mx8(dtype, src, rows, cols, q, scale, (hipStream_t)stream), __func__);
 }
 
+int unipool_mx8_form(const unipool_shape* shape) {
+    PROLOGUE();
+    if (shape->dtype != UNIPOOL_BF16)
+        return set_error(UNIPOOL_EINVAL, "%s: experts in 8 bits exist in bfloat16 mode only", __func__);
+    return mx8_ffn_form(*shape);
+}
+
 int unipool_expert_ffn_fwd_mx8(const unipool_shape* shape, const void* x_q, const void* x_scale, const int32_t* slot_of_row,
                                const int32_t* expert_offsets, const void* w_gate_up_q, const void* w_gate_up_scale,
                                const void* w_down_q, const void* w_down_scale, void* h_q, void* h_scale, void* y_perm,

@@ -696,6 +696,11 @@ template <bool GATE_UP> hipError_t run_few_mx8(const unipool_shape& s, const Mx8
 
 }  // namespace
 
+int mx8_ffn_form(const unipool_shape& s) {
+    constexpr int kForms[] = {0, 64128, 96128, 64256, 128256, 192256};
+    return kForms[mx8_form(s)];
+}
+
 hipError_t mx8_ffn_fwd(const unipool_shape& s, const void* x, const void* x_scale, const int32_t* slot_of_row, const int32_t* offsets,
                        const void* wgu, const void* wgu_scale, const void* wd, const void* wd_scale, void* h, void* h_scale, void* y,
                        hipStream_t st) {

@@ -37,6 +37,9 @@ class LayerState:
     dx: Optional[torch.Tensor] = None
     d_w_router: Optional[torch.Tensor] = None
     d_sigma: Optional[torch.Tensor] = None
+    # balance loss over sequences: gradients of the logits and of sigma
+    seq_d_logits: Optional[torch.Tensor] = None
+    seq_d_sigma: Optional[torch.Tensor] = None
 
 
 class PoolStep:
@@ -56,10 +59,15 @@ class PoolStep:
     router    "norm": the NormRouter of Eq. 7; "softmax": the softmax router of the comparison rows (Sec. 5.4).
     lagged    App. G (pool auxiliary loss derivation), one-step-behind: micro-batch m uses the usage statistic fbar of micro-batch
               m-1, held constant; the first micro-batch uses its own.  The statistic lives in two
-              device buffers used in turn and is part of state_dict()."""
+              device buffers used in turn and is part of state_dict().
+    n_seq     balance loss over sequences beside `aux`: the batch is cut into n_seq sequences at seq_offsets (device, [n_seq + 1];
+              evenly at first, set_sequences changes it), every layer adds unipool_seq_balance_loss with coefficient seq_alpha, each
+              with weight one.  Losses are in seq_loss[L], picks per sequence in seq_counts[L, n_seq, E]."""
 
     def __init__(self, T, d_model, d_ff, E, k, L, dtype, c, eps, alpha_pool, device="cuda:0",
-                 wgrad="pool", recompute=False, lagged=False, aux="pool", router="norm", wgrad_layers=None):
+                 wgrad="pool", recompute=False, lagged=False, aux="pool", router="norm", wgrad_layers=None,
+                 n_seq=None, seq_alpha=0.0):
+        assert n_seq is None or n_seq >= 1
         assert wgrad_layers is None or (wgrad == "layer" and wgrad_layers >= 1)
         assert wgrad in ("pool", "layer") and aux in ("pool", "layer") and router in ("norm", "softmax")
         self.router = B.ROUTER_SOFTMAX if router == "softmax" else B.ROUTER_NORM
@@ -93,6 +101,11 @@ class PoolStep:
             self.aux_coef_layers = torch.zeros((L, E), **f32)
             self.f_layers = torch.zeros((L, E), **f32)
             self._pool_counts_layers = torch.zeros((L, E), **i32)
+        self.n_seq, self.seq_alpha = n_seq, float(seq_alpha)
+        if n_seq is not None:
+            self.seq_offsets = torch.tensor([T * b // n_seq for b in range(n_seq + 1)], **i32)
+            self.seq_counts = torch.zeros((L, n_seq, E), **i32)
+            self.seq_loss = torch.zeros(L, **f32)
         self.layers: List[LayerState] = []
         shared_ab = (torch.empty((S, f), **act), torch.empty((S, f), **act)) if self.recompute else None
         for _ in range(L):
@@ -109,6 +122,8 @@ class PoolStep:
             st.dx = torch.empty((T, d), **act)
             st.d_w_router = torch.empty((E, d), **f32)
             st.d_sigma = torch.empty(1, **f32)
+            if n_seq is not None:
+                st.seq_d_logits, st.seq_d_sigma = torch.empty((T, E), **f32), torch.empty(1, **f32)
             self.layers.append(st)
         # backward buffers: per layer when the weight gradient is deferred, otherwise for one layer until the first step()
         self._dy, self._dact = [], []
@@ -179,6 +194,9 @@ class PoolStep:
         of x through slot_of_row).  The backward pass needs x_perm, so a training step leaves it off."""
         st, sh, ws = self.layers[l], self.shape(sigma), self.ws
         self._call(B.route, sh, x, w_router, st.topk_idx, st.topk_gate, st.logits, self.counts[l], self.psum[l], ws)
+        if self.n_seq is not None:                       # the picks of the layer are all it needs
+            self._call(B.seq_balance_loss, sh, self.n_seq, self.seq_offsets, self.seq_alpha, st.logits, st.topk_idx, self.seq_counts[l],
+                       self.seq_loss[l:l + 1], st.seq_d_logits, st.seq_d_sigma, ws)
         self._call(B.permute, sh, None if gather else x, st.topk_idx, self.counts[l], None if gather else st.x_perm,
                    st.offsets, st.row_of_slot, st.slot_of_row, ws)
         if gather:
@@ -211,6 +229,12 @@ class PoolStep:
         self.fbar = out
         self.micro_batches_done += 1
         return self.loss
+
+    def set_sequences(self, offsets):
+        """First token of every sequence, and the end of the last one (n_seq + 1 numbers that do not decrease; a sequence may be
+        empty, and tokens in front of the first or behind the last count as padding)."""
+        assert self.n_seq is not None and len(offsets) == self.n_seq + 1
+        self.seq_offsets.copy_(torch.as_tensor(offsets, dtype=torch.int32))
 
     def state_dict(self):
         """What a checkpoint of the micro-batch loop has to hold."""
@@ -245,8 +269,12 @@ class PoolStep:
                          self._dxp, dact, dwgu, dwd, ws)
         self._call(B.combine, sh, self._dxp, st.row_of_slot, None, st.dx, ws)            # backward of the dispatch
         coef = self.aux_coef if self.aux == "pool" else self.aux_coef_layers[l]
-        self._call(B.route_bwd, sh, x, w_router, st.logits, st.topk_idx, st.dgate, coef, st.d_w_router,
-                    st.d_sigma, st.dx, True, ws)
+        if self.n_seq is not None:
+            self._call(B.route_bwd_add, sh, x, w_router, st.logits, st.topk_idx, st.dgate, coef, st.seq_d_logits, st.seq_d_sigma,
+                       st.d_w_router, st.d_sigma, st.dx, True, ws)
+        else:
+            self._call(B.route_bwd, sh, x, w_router, st.logits, st.topk_idx, st.dgate, coef, st.d_w_router,
+                       st.d_sigma, st.dx, True, ws)
         return st.dx
 
     def _add_wgrad(self, group, accumulate):
@@ -303,3 +331,114 @@ class PoolGroups:
         for g, ps in enumerate(self.groups):
             lo, hi = g * self.Lg, (g + 1) * self.Lg
             ps.step(xs[lo:hi], w_routers[lo:hi], sigmas[lo:hi], w_gate_up[g], w_down[g], grad_outs[lo:hi])
+
+
+class PoolStack:
+    """The L layers of a PoolStep as the FFN sub-layers of a pre-norm transformer:
+        h_0 = x;   y_l = norm(h_l);   h_{l+1} = h_l + layer_l(y_l);   result: y_L = norm(h_L).
+    norm_weights: [d] act tensors, L + 1 of them, the last for the result.  The residual's addition is part of the next layer's
+    norm (unipool_rmsnorm), and backward the gradient of the residual path part of the norm's (unipool_rmsnorm_bwd).  Gradients of the
+    norm weights are in d_norm[L + 1, d] (float), those of everything else in the PoolStep."""
+
+    def __init__(self, step: PoolStep, norm_eps=1e-6):
+        self.step, self.norm_eps = step, float(norm_eps)
+        act = dict(dtype=step.act, device=step.dev)
+        T, d, L = step.T, step.d, step.L
+        self.h = [None] + [torch.empty((T, d), **act) for _ in range(L)]      # h[0]: the caller's x
+        self.y = [torch.empty((T, d), **act) for _ in range(L + 1)]
+        self.dx = torch.empty((T, d), **act)
+        self.d_norm = torch.empty((L + 1, d), dtype=torch.float32, device=step.dev)
+
+    def forward(self, x, norm_weights, w_routers, sigmas, w_gate_up, w_down, fbar_in=None):
+        ps = self.step
+        self.h[0] = x
+        sh = ps.shape(1.0)
+        ps._call(B.rmsnorm, sh, x, None, norm_weights[0], self.norm_eps, None, self.y[0], None, None)
+        for l in range(ps.L):
+            out = ps.forward_layer(l, self.y[l], w_routers[l], sigmas[l], w_gate_up, w_down)
+            ps._call(B.rmsnorm, sh, out, self.h[l], norm_weights[l + 1], self.norm_eps, self.h[l + 1], self.y[l + 1], None, None)
+        ps.aux_loss(fbar_in)
+        return self.y[ps.L]
+
+    def backward(self, grad_y, norm_weights, w_routers, sigmas, w_gate_up, w_down):
+        """Returns the gradient of x; the objective is <grad_y, y_L> plus the auxiliary losses."""
+        ps, dx = self.step, self.dx
+        sh = ps.shape(1.0)
+        ps.begin_backward()
+        # dx: the gradient of h_{l+1}, which is that of layer l's output and, along the residual, of h_l
+        ps._call(B.rmsnorm_bwd, sh, self.h[ps.L], norm_weights[ps.L], grad_y, None, self.norm_eps, dx, self.d_norm[ps.L], ps.ws)
+        for l in reversed(range(ps.L)):
+            dy = ps.backward_layer(l, self.y[l], w_routers[l], sigmas[l], w_gate_up, w_down, dx)
+            ps._call(B.rmsnorm_bwd, sh, self.h[l], norm_weights[l], dy, dx, self.norm_eps, dx, self.d_norm[l], ps.ws)
+        ps.end_backward()
+        return dx
+
+
+class PoolServe:
+    """Forward pass of the same stack for serving, the pool's experts in 8 bits (MX8): the norm in front of a layer writes its rows for the
+    router (act) and for the experts (8 bits), which read them through slot_of_row.  bfloat16; up to T tokens a call.
+
+    w_gate_up [E, 2 d_ff, d], w_down [E, d, d_ff]: the pool's weights (bfloat16), laid out in 8 bits here, once."""
+
+    def __init__(self, T, d_model, d_ff, E, k, c, eps, w_gate_up, w_down, router="norm", norm_eps=1e-6):
+        assert router in ("norm", "softmax")
+        assert w_gate_up.shape == (E, 2 * d_ff, d_model) and w_down.shape == (E, d_model, d_ff)
+        assert w_gate_up.dtype == w_down.dtype == torch.bfloat16
+        self.T, self.d, self.f, self.E, self.k = T, d_model, d_ff, E, k
+        self.c, self.eps, self.norm_eps = c, eps, float(norm_eps)
+        self.router = B.ROUTER_SOFTMAX if router == "softmax" else B.ROUTER_NORM
+        self.dev = w_gate_up.device
+        self.ws = torch.empty(B.workspace_bytes(self.shape(T, 1.0)), dtype=torch.uint8, device=self.dev)
+        self.w_gate_up = self._mx8(E * 2 * d_ff, d_model)
+        self.w_down = self._mx8(E * d_model, d_ff)
+        B.quantize_mx8(B.BF16, E * 2 * d_ff, d_model, w_gate_up, *self.w_gate_up)
+        B.quantize_mx8(B.BF16, E * d_model, d_ff, w_down, *self.w_down)
+        i32 = dict(dtype=torch.int32, device=self.dev)
+        f32 = dict(dtype=torch.float32, device=self.dev)
+        act = dict(dtype=torch.bfloat16, device=self.dev)
+        S = T * k
+        self.residual, self.y, self.out = (torch.empty((T, d_model), **act) for _ in range(3))
+        self.x_q, self.h_q = self._mx8(T, d_model), self._mx8(S, d_ff)
+        self.y_perm = torch.empty((S, d_model), **act)
+        self.topk_idx, self.topk_gate = torch.empty((T, k), **i32), torch.empty((T, k), **f32)
+        self.logits = torch.empty((T, E), **f32)
+        self.counts, self.psum = torch.empty(E, **i32), torch.empty(E, **f32)
+        self.offsets, self.row_of_slot, self.slot_of_row = torch.empty(E + 1, **i32), torch.empty((T, k), **i32), torch.empty(S, **i32)
+
+    def _mx8(self, rows, cols):
+        u8 = dict(dtype=torch.uint8, device=self.dev)
+        return torch.empty((rows, cols), **u8), torch.empty(B.mx8_scale_shape(rows, cols), **u8)
+
+    def shape(self, T, sigma) -> B.Shape:
+        return B.Shape(T, self.d, self.f, self.E, self.k, 1, B.BF16, float(sigma), self.c, self.eps, 0.0, self.router)
+
+    def layer(self, x, residual, h, norm_weight, w_router, sigma):
+        """One sub-layer for x.shape[0] tokens: h = x + residual (residual None: h = x, and h may be None), returns the layer's output of
+        norm(h).  The output stays valid until the next call."""
+        n = x.shape[0]
+        assert 1 <= n <= self.T and x.shape[1] == self.d
+        sh, ws = self.shape(n, sigma), self.ws
+        # (the first n rows of a buffer; scales of n rows are packed anew, since their layout goes by the number of rows)
+        xs = self.x_q[1].view(-1)[:4 * n * -(-self.d // 128)]
+        hs = self.h_q[1].view(-1)[:4 * n * self.k * -(-self.f // 128)]
+        y, out, idx, gate, ros = self.y[:n], self.out[:n], self.topk_idx[:n], self.topk_gate[:n], self.row_of_slot[:n]
+        B.rmsnorm(sh, x, residual, norm_weight, self.norm_eps, h, y, self.x_q[0], xs)
+        B.route(sh, y, w_router, idx, gate, self.logits[:n], self.counts, self.psum, ws)
+        B.permute(sh, None, idx, self.counts, None, self.offsets, ros, self.slot_of_row, ws)
+        B.expert_ffn_fwd_mx8(sh, self.x_q[0], xs, self.slot_of_row, self.offsets, *self.w_gate_up, *self.w_down, self.h_q[0], hs,
+                             self.y_perm, ws)
+        B.combine(sh, self.y_perm, ros, gate, out)
+        return out
+
+    def forward(self, x, norm_weights, w_routers, sigmas):
+        """All layers (as many as there are routers) and the final norm, as PoolStack.forward; x is left as it is."""
+        n, h = x.shape[0], None
+        for l, (w_router, sigma) in enumerate(zip(w_routers, sigmas)):
+            if l == 0:
+                out = self.layer(x, None, None, norm_weights[0], w_router, sigma)
+                h = x
+            else:
+                out = self.layer(out, h, self.residual[:n], norm_weights[l], w_router, sigma)
+                h = self.residual[:n]
+        B.rmsnorm(self.shape(n, 1.0), out, h, norm_weights[len(w_routers)], self.norm_eps, None, self.y[:n], None, None)
+        return self.y[:n]

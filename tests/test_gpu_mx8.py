@@ -126,7 +126,19 @@ SIZES = [
 ]
 
 
-@pytest.mark.parametrize("T,E,d,f,k,skew", SIZES)
+# every form: weights streamed to registers, and the tiles (rows and weight rows)
+FORMS = {0: [SIZES[0], SIZES[3], SIZES[6]], 64128: [SIZES[5], SIZES[7], SIZES[8], SIZES[14]], 96128: [SIZES[9], SIZES[11], SIZES[15]],
+         128256: [(1600, 16, 64, 8192, 1, "none")], 192256: [(3300, 16, 64, 4160, 1, "none"), (3300, 16, 192, 4160, 1, "hot")]}
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_sizes_take_every_form(form):
+    U = lib()
+    for T, E, d, f, k, _ in FORMS[form]:
+        assert U.mx8_form(U.Shape(T=T, d_model=d, d_ff=f, E=E, k=k, L=1, dtype=U.BF16, sigma=1.0, c=2.5, eps=1e-6, alpha_pool=0.01)) == form
+
+
+@pytest.mark.parametrize("T,E,d,f,k,skew", SIZES + FORMS[128256] + FORMS[192256])
 def test_experts(T, E, d, f, k, skew):
     import torch
     off, ros, sor = routing(T, E, k, T + E, skew)
@@ -221,3 +233,32 @@ def test_recorded_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("d,f,expected", [(64, 8192, [0, 64128, 64128, 128256, 192256, 192256]), (320, 8256, [64128, 64128, 64256, 128256, 192256, 192256])])
+def test_forms_agree_bit_for_bit(d, f, expected):
+    """A token's rows do not depend on how many tokens share the call, nor on the form that many take: the same first tokens in calls of
+    growing size, with gathered rows whose numbers pass through LDS (several stages) and without."""
+    import torch
+    U, E, k = lib(), 64, 2
+    T_all = 9000
+    off, ros, sor = routing(T_all, E, k, 6, "none")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    qs = []
+    for rows, cols, std in ((T_all, d, 1.0), (E * 2 * f, d, 0.05), (E * d, f, 0.05)):
+        v = torch.randn((rows, cols), generator=g, device="cuda") * std
+        q = new_mx8(rows, cols)
+        U.quantize_mx8(U.F32, rows, cols, v, *q)
+        qs.append(q)
+    idx = np.empty((T_all, k), np.int64)                     # the experts of every token, from the permutation
+    idx.reshape(-1)[sor] = np.repeat(np.arange(E), np.diff(off))
+    first, forms = None, []
+    for T in (1, 3, 700, 2400, 3600, T_all):
+        o, r, s = P.permutation(idx[:T], E)
+        xq = (qs[0][0][:T].contiguous(), qs[0][1][:, :T].contiguous())
+        forms.append(U.mx8_form(U.Shape(T=T, d_model=d, d_ff=f, E=E, k=k, L=1, dtype=U.BF16, sigma=1.0, c=2.5, eps=1e-6, alpha_pool=0.01)))
+        _, y = run(T, E, d, f, k, [xq, *qs[1:]], o, s)
+        mine = y[torch.from_numpy(r[:1].reshape(-1).astype(np.int64)).cuda()]
+        first = mine if first is None else first
+        assert torch.equal(mine, first), (T, forms[-1])
+    assert forms == expected
