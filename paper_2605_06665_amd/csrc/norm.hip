@@ -2,6 +2,7 @@
 //
 //   h = x + r;  s = 1 / sqrt(mean(h^2) + eps);  y = h s w
 //   g = w dy;   dx = s g - h s^3 mean(g h) + dh;   dw = sum over the rows of dy h s
+// (h s is of order one and is formed first: s^3 alone would pass the largest float where rows are of order 1e-13 and eps is 0)
 //
 // Both passes are bound by memory: a row is read once, held in registers as it came, and every output leaves from there.  A
 // value takes a handful of operations, all in float; h is rounded only where it is stored, and y, in 16 or in 8 bits, is made
@@ -78,6 +79,7 @@ struct NormArgs {
     unsigned char *q, *scale;
     int T, d;
     float eps;
+    int row0;                 // first row of the launch
 };
 
 // W wavefronts share a row and hold it in R chunks of N values a lane.
@@ -87,7 +89,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rmsnorm_kernel(const No
     constexpr int kRows = W == 1 ? 4 : 1;                  // rows of a workgroup
     __shared__ float red[W];
     const int lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
-    const size_t row = (size_t)blockIdx.x * kRows + (W == 1 ? threadIdx.x >> 6 : 0);
+    const size_t row = a.row0 + (size_t)blockIdx.x * kRows + (W == 1 ? threadIdx.x >> 6 : 0);
     if (row >= (size_t)a.T) return;
     const int d = a.d;
     const size_t o = row * d;
@@ -200,7 +202,7 @@ __global__ __launch_bounds__(W == 1 ? 64 * kBwdRows : 64 * W) void rmsnorm_bwd_k
         ss = row_sum<W>(ss, red[0]);
         sg = row_sum<W>(sg, red[1]);
         const float rs = 1.0f / sqrtf(ss / (float)d + a.eps);
-        const float back = rs * rs * rs * (sg / (float)d);
+        const float back = rs * (rs * (sg / (float)d));
 #pragma unroll
         for (int i = 0; i < R; i++) {
             const int c = i * STEP + lane * N;
@@ -211,9 +213,10 @@ __global__ __launch_bounds__(W == 1 ? 64 * kBwdRows : 64 * W) void rmsnorm_bwd_k
             if (a.dh != nullptr) unpack<TA, N>(ep[i], e);
 #pragma unroll
             for (int j = 0; j < N; j++) {
-                float v = rs * (q[j] * g[j]) - h[j] * back;
+                const float hs = h[j] * rs;
+                float v = rs * (q[j] * g[j]) - hs * back;
                 if (a.dh != nullptr) v += e[j];
-                dw[i][j] += g[j] * (h[j] * rs);
+                dw[i][j] += g[j] * hs;
                 q[j] = v;
             }
             if (c < d) *reinterpret_cast<P*>((TA*)a.dx + o + c) = pack<TA, N>(q);
@@ -308,11 +311,16 @@ bool aligned16(std::initializer_list<const void*> ps) {
 }
 
 template <typename TA>
-hipError_t run_norm(const NormArgs& a, hipStream_t st) {
-    constexpr int n = 16 / sizeof(TA);
+hipError_t run_norm(NormArgs a, hipStream_t st) {
+    constexpr int n = 16 / sizeof(TA), kRowsPerLaunch = 1 << 21;      // a launch has less than 2^32 threads, and a row up to 1024
+    const int T = a.T;
     const bool wide = a.d % n == 0 && aligned16({a.x, a.residual, a.weight, a.h, a.y}) && ((uintptr_t)a.q & 7) == 0;
     with_norm_form<TA>(a.d, wide, [&](auto nn, auto w, auto r) {
-        rmsnorm_kernel<TA, nn(), w(), r()><<<w() == 1 ? cdiv(a.T, 4) : a.T, w() == 1 ? 256 : 64 * w(), 0, st>>>(a);
+        for (long long row0 = 0; row0 < T; row0 += kRowsPerLaunch) {
+            const int rows = (int)std::min<long long>(T - row0, kRowsPerLaunch);
+            a.row0 = (int)row0;
+            rmsnorm_kernel<TA, nn(), w(), r()><<<w() == 1 ? cdiv(rows, 4) : rows, w() == 1 ? 256 : 64 * w(), 0, st>>>(a);
+        }
     });
     return hipGetLastError();
 }
@@ -337,7 +345,7 @@ hipError_t run_norm_bwd(NormBwdArgs a, float* d_weight, float* part, hipStream_t
 
 hipError_t launch_rmsnorm(const unipool_shape& s, const void* x, const void* residual, const void* weight, float eps, void* h,
                           void* y, void* y_q, void* y_scale, hipStream_t st) {
-    const NormArgs a = {x, residual, weight, h, y, (unsigned char*)y_q, (unsigned char*)y_scale, s.T, s.d_model, eps};
+    const NormArgs a = {x, residual, weight, h, y, (unsigned char*)y_q, (unsigned char*)y_scale, s.T, s.d_model, eps, 0};
     return s.dtype == UNIPOOL_BF16 ? run_norm<bf16>(a, st) : run_norm<float>(a, st);
 }
 

@@ -207,3 +207,37 @@ def test_recorded_and_replayed_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((h, y, q, s, dx, dw), want))
+
+
+@pytest.mark.parametrize("dtype,T,d", [("bf16", 9, 192), ("bf16", 3, 4160), ("f32", 9, 96), ("f32", 3, 33)])
+def test_backward_of_tiny_rows_without_eps(dtype, T, d):
+    """s is 1e15 here: s^3 is beyond the largest float, the gradient is not."""
+    import torch
+    U, sh = lib(), shape(T, d, dtype)
+    h, dy = rows(T, d, dtype, 21, 1e-15), rows(T, d, dtype, 22)
+    w = round_act(1.0 + 0.1 * np.random.default_rng(23).standard_normal(d), dtype)
+    dx_ref, dw_ref = O.rmsnorm_bwd(h, w, dy, None, 0.0)
+    ws = torch.full((U.workspace_bytes(sh),), 255, dtype=torch.uint8, device="cuda")
+    dx, dw = like(dev(h, dtype)), torch.full((d,), float("nan"), device="cuda")
+    U.rmsnorm_bwd(sh, dev(h, dtype), dev(w, dtype), dev(dy, dtype), None, 0.0, dx, dw, ws)
+    s = 1.0 / np.sqrt(np.mean(h.astype(np.float64) ** 2, axis=1, keepdims=True))
+    g = np.abs(w * dy.astype(np.float64))
+    mag = s * g + np.abs(h) * s ** 3 * np.mean(g * np.abs(h), axis=1, keepdims=True)
+    assert act_err(host(dx), dx_ref, dtype, C * mag) <= 1
+    assert (np.abs(host(dw) - dw_ref) <= 2 * C * np.sum(np.abs(dy.astype(np.float64) * h * s), axis=0)).all()
+
+
+def test_more_rows_than_a_launch_takes():
+    """2^21 rows go in one launch; every row is a call of its own as far as its bits go."""
+    import torch
+    U, d = lib(), 32
+    T = 2 * (1 << 21) + 5
+    x = torch.randn(T, d, device="cuda")
+    w = torch.randn(d, device="cuda")
+    y, (q, s) = like(x), mx8_of(T, d)
+    U.rmsnorm(shape(T, d, "f32"), x, None, w, EPS, None, y, q, s)
+    for lo, hi in ((0, 1 << 20), (1 << 20, (1 << 21) + 7), ((1 << 21) + 7, 1 << 22), ((1 << 22) - 3, T)):
+        n = hi - lo
+        y2, (q2, s2) = like(x[lo:hi]), mx8_of(n, d)
+        U.rmsnorm(shape(n, d, "f32"), x[lo:hi].clone(), None, w, EPS, None, y2, q2, s2)
+        assert torch.equal(y2, y[lo:hi]) and torch.equal(q2, q[lo:hi]) and torch.equal(s2, s[:, lo:hi])
