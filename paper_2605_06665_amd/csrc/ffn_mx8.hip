@@ -67,7 +67,9 @@ __device__ __forceinline__ void store_h(const Mx8Args& a, const f32x4& a0, const
     unsigned char* dst = a.h + row * a.N + col + 4 * lg;
     *reinterpret_cast<unsigned*>(dst) = mx8_pack4(h[0], h[1], h[2], h[3], byte);
     *reinterpret_cast<unsigned*>(dst + 16) = mx8_pack4(h[4], h[5], h[6], h[7], byte);
-    if (lg == 0) a.h_scale[mx8_scale_at(a.S, row, col / kMxBlock)] = (unsigned char)byte;
+    unsigned char* const sc = a.h_scale + mx8_scale_at(a.S, row, col / kMxBlock);
+    if (lg == 0) *sc = (unsigned char)byte;
+    if (col + kMxBlock == a.N && a.N % kMxStep != 0 && lg == 1) *reinterpret_cast<unsigned short*>(sc + 1) = kMxBias * 0x101;      // the word's rest
 }
 
 // What a reduction whose length is no multiple of 128 reads past its end.  Never written.

@@ -262,3 +262,26 @@ def test_forms_agree_bit_for_bit(d, f, expected):
         first = mine if first is None else first
         assert torch.equal(mine, first), (T, forms[-1])
     assert forms == expected
+
+
+@pytest.mark.parametrize("T,E,d,f,k", [(4, 6, 64, 192, 2), (1, 1, 64, 64, 1), (200, 5, 128, 320, 2), (130, 3, 64, 448, 1)])
+def test_scale_bytes_past_the_columns_of_h(T, E, d, f, k):
+    off, ros, sor = routing(T, E, k, 3, "none")
+    (_, hs), _ = run(T, E, d, f, k, case(T, E, d, f, k, "none"), off, sor)
+    last = hs[-1].cpu().numpy()
+    assert (last[:, f % 128 // 32:] == 127).all() and (last[:, :f % 128 // 32] != 255).all()
+
+
+@pytest.mark.parametrize("T", [5, 300])
+def test_rows_outside_the_offsets_are_left_alone(T):
+    import torch
+    E, d, f, k = 4, 128, 192, 2
+    off, ros, sor = routing(T, E, k, 4, "none")
+    qs = case(T, E, d, f, k, "none")
+    (hq, hs), y = run(T, E, d, f, k, qs, off, sor, gathered=False)
+    lo, hi = int(off[1]), int(off[3])                      # the first and the last expert get none of their rows
+    cut = np.clip(off, lo, hi)
+    (hq2, hs2), y2 = run(T, E, d, f, k, qs, cut, sor, gathered=False)
+    assert torch.equal(hq2[lo:hi], hq[lo:hi]) and torch.equal(hs2[:, lo:hi], hs[:, lo:hi]) and torch.equal(y2[lo:hi], y[lo:hi])
+    for r in (slice(0, lo), slice(hi, None)):
+        assert (hq2[r] == 0x55).all() and (hs2[:, r] == 255).all() and torch.isnan(y2[r]).all()
