@@ -178,9 +178,18 @@ __global__ __launch_bounds__(kLossThreads) void seq_loss_kernel(const SeqArgs a)
     for (int tw = t0; tw < end; tw += TPW) {
         const int t = tw + grp;
         const bool live = t < end;
-        while (b < a.n_seq && s1 <= t) {
+        if (b < a.n_seq && s1 <= t) {                // mostly the next one; behind many empty ones it is looked for
             b++;
             if (b < a.n_seq) seq_range(a, b, s0, s1);
+            if (b < a.n_seq && s1 <= t) {
+                int hi = a.n_seq;
+                for (b++; b < hi;) {
+                    const int mid = b + (hi - b) / 2;
+                    if (a.offsets[mid + 1] > t) hi = mid;
+                    else b = mid + 1;
+                }
+                if (b < a.n_seq) seq_range(a, b, s0, s1);
+            }
         }
         const bool in = live && b < a.n_seq && t >= s0;
         if (in && have != b) {

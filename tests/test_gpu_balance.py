@@ -175,3 +175,11 @@ def test_one_workgroup_and_several(T, E, n_seq):
     off = np.sort(np.random.default_rng(n_seq).integers(0, T + 1, n_seq + 1)).astype(np.int32)
     for router in ("norm", "softmax"):
         check(T, E, k, router, z, off, run(T, E, k, router, z, picks(z, k), off))
+
+
+@pytest.mark.parametrize("router", ["norm", "softmax"])
+def test_many_empty_sequences_between_those_with_tokens(router):
+    T, E, k = 310, 16, 2
+    z = np.random.default_rng(12).standard_normal((T, E)).astype(np.float32)
+    off = [0] * 700 + [1, 2, 2, 3] + [7] * 1500 + [100] * 3 + [101, 150] + [151] * 900 + [300] * 2
+    check(T, E, k, router, z, off, run(T, E, k, router, z, picks(z, k), off))
