@@ -351,6 +351,7 @@ class PoolStack:
 
     def forward(self, x, norm_weights, w_routers, sigmas, w_gate_up, w_down, fbar_in=None):
         ps = self.step
+        assert x.data_ptr() != self.y[ps.L].data_ptr(), "x is kept for the backward pass; this call overwrites it with its result"
         self.h[0] = x
         sh = ps.shape(1.0)
         ps._call(B.rmsnorm, sh, x, None, norm_weights[0], self.norm_eps, None, self.y[0], None, None)
@@ -397,7 +398,7 @@ class PoolServe:
         f32 = dict(dtype=torch.float32, device=self.dev)
         act = dict(dtype=torch.bfloat16, device=self.dev)
         S = T * k
-        self.residual, self.y, self.out = (torch.empty((T, d_model), **act) for _ in range(3))
+        self.residual, self.y, self.out, self.result = (torch.empty((T, d_model), **act) for _ in range(4))
         self.x_q, self.h_q = self._mx8(T, d_model), self._mx8(S, d_ff)
         self.y_perm = torch.empty((S, d_model), **act)
         self.topk_idx, self.topk_gate = torch.empty((T, k), **i32), torch.empty((T, k), **f32)
@@ -416,7 +417,7 @@ class PoolServe:
         """One sub-layer for x.shape[0] tokens: h = x + residual (residual None: h = x, and h may be None), returns the layer's output of
         norm(h).  The output stays valid until the next call."""
         n = x.shape[0]
-        assert 1 <= n <= self.T and x.shape[1] == self.d
+        assert 1 <= n <= self.T and x.shape == (n, self.d) and x.dtype == torch.bfloat16
         sh, ws = self.shape(n, sigma), self.ws
         # (the first n rows of a buffer; scales of n rows are packed anew, since their layout goes by the number of rows)
         xs = self.x_q[1].view(-1)[:4 * n * -(-self.d // 128)]
@@ -431,7 +432,9 @@ class PoolServe:
         return out
 
     def forward(self, x, norm_weights, w_routers, sigmas):
-        """All layers (as many as there are routers) and the final norm, as PoolStack.forward; x is left as it is."""
+        """All layers (as many as there are routers) and the final norm, as PoolStack.forward; x is left as it is.  The result stays
+        valid until the next call, which may take it as its x."""
+        assert len(w_routers) == len(sigmas) == len(norm_weights) - 1 >= 1
         n, h = x.shape[0], None
         for l, (w_router, sigma) in enumerate(zip(w_routers, sigmas)):
             if l == 0:
@@ -440,5 +443,5 @@ class PoolServe:
             else:
                 out = self.layer(out, h, self.residual[:n], norm_weights[l], w_router, sigma)
                 h = self.residual[:n]
-        B.rmsnorm(self.shape(n, 1.0), out, h, norm_weights[len(w_routers)], self.norm_eps, None, self.y[:n], None, None)
-        return self.y[:n]
+        B.rmsnorm(self.shape(n, 1.0), out, h, norm_weights[len(w_routers)], self.norm_eps, None, self.result[:n], None, None)
+        return self.result[:n]

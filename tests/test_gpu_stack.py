@@ -188,3 +188,35 @@ def test_serving_in_8_bits(T, n, d, f, E, k, L, router):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(yg, want)
+
+
+def test_serving_takes_its_own_result_and_refuses_what_does_not_fit():
+    import torch
+    from paper_2605_06665_amd.pipeline import PoolServe
+    T, d, f, E, k, L = 20, 128, 64, 4, 2, 2
+    i = inputs(T, d, f, E, L, "bf16", 5)
+    sv = PoolServe(T, d, f, E, k, C, EPS, dev(np.concatenate([i["wg"], i["wu"]], axis=1), "bf16"), dev(i["wd"], "bf16"), norm_eps=NORM_EPS)
+    norms, wrs = [dev(w, "bf16") for w in i["norms"]], [dev(w, "bf16") for w in i["wrs"]]
+    x = dev(i["x"], "bf16")
+    first = sv.forward(x, norms, wrs, i["sigmas"]).clone()
+    want = sv.forward(first, norms, wrs, i["sigmas"]).clone()
+    assert torch.equal(sv.forward(sv.forward(x, norms, wrs, i["sigmas"]), norms, wrs, i["sigmas"]), want)
+    for bad in (lambda: sv.forward(x, norms, [], []), lambda: sv.forward(x, norms, wrs, i["sigmas"][:1]), lambda: sv.forward(x, norms[:L], wrs, i["sigmas"]),
+                lambda: sv.forward(x.float(), norms, wrs, i["sigmas"]), lambda: sv.forward(torch.cat([x, x]), norms, wrs, i["sigmas"])):
+        with pytest.raises(AssertionError):
+            bad()
+
+
+def test_stack_refuses_its_result_as_its_input():
+    import torch
+    from paper_2605_06665_amd.pipeline import PoolStack, PoolStep
+    from paper_2605_06665_amd import binding as B
+    T, d, f, E, k, L = 20, 64, 64, 4, 2, 1
+    i = inputs(T, d, f, E, L, "bf16", 6)
+    stack = PoolStack(PoolStep(T, d, f, E, k, L, B.BF16, C, EPS, 0.01), NORM_EPS)
+    args = ([dev(w, "bf16") for w in i["norms"]], [dev(w, "bf16") for w in i["wrs"]], i["sigmas"], dev(np.concatenate([i["wg"], i["wu"]], axis=1), "bf16"),
+            dev(i["wd"], "bf16"))
+    y = stack.forward(dev(i["x"], "bf16"), *args)
+    with pytest.raises(AssertionError, match="kept for the backward"):
+        stack.forward(y, *args)
+    torch.cuda.synchronize()
