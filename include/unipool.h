@@ -327,8 +327,8 @@ int unipool_seq_balance_loss(const unipool_shape* shape, int n_seq, const int32_
 /*
  * Root-mean-square norm of the rows in front of a layer, with the addition of the residual.
  *   h = x + residual (h = x if residual is NULL);   y = h / sqrt(mean(h^2) + norm_eps) * weight
- * All of it in float; y is made from the unrounded h.  y may leave as act, in 8 bits (MX8, below), or both: the router reads the
- * one, unipool_expert_ffn_fwd_mx8 the other.
+ * All of it in float, whose range also holds for the sum of h^2; y is made from the unrounded h.  y may leave as act, in 8 bits
+ * (MX8, below), or both: the router reads the one, unipool_expert_ffn_fwd_mx8 the other.
  * in : x [T, d] act;  residual [T, d] act or NULL;  weight [d] act;  norm_eps >= 0;  d <= 16384.
  * out: h [T, d] act or NULL (may be x or residual itself);  y [T, d] act or NULL;  y_q [T, d] and y_scale in MX8, or both NULL
  *      (needs d to be a multiple of 32).  One of y and y_q must be given.
@@ -355,7 +355,7 @@ int unipool_rmsnorm_bwd(const unipool_shape* shape, const void* h, const void* w
  * unipool_quantize_mx8 lays a matrix out so, e.g. once the weights of the pool: w_gate_up as 2 d_ff E rows of d_model,
  * w_down as d_model E rows of d_ff.
  * in : src [rows, cols] float (dtype UNIPOOL_F32) or bfloat16 (UNIPOOL_BF16);  cols a multiple of 32;
- *      ceil(rows / 64) * ceil(cols / 128) < 2^31.
+ *      ceil(rows / 64) * ceil(cols / 128) < 2^24.
  * out: q [rows, cols] bytes;  scale [ceil(cols / 128), rows, 4] bytes.
  */
 int unipool_quantize_mx8(int dtype, long long rows, int cols, const void* src, void* q, void* scale, void* stream);
@@ -367,7 +367,8 @@ int unipool_quantize_mx8(int dtype, long long rows, int cols, const void* src, v
  * in : x_q, x_scale: the tokens [T, d] in MX8 when slot_of_row is given (row r of the group order is token slot_of_row[r] / k), or the
  *      rows [S, d] in group order when it is NULL;  expert_offsets [E+1];  w_gate_up_q [E, 2 d_ff, d], w_down_q [E, d, d_ff] with
  *      their scales.  The values, the weights' scales and y_perm must be aligned to 16 bytes, the other scales to 4; d, d_ff <= 2^20.
- * out: h_q [S, d_ff], h_scale (H in MX8);  y_perm [S, d] bfloat16.
+ * out: h_q [S, d_ff], h_scale (H in MX8);  y_perm [S, d] bfloat16.  Rows in front of expert_offsets[0] and from expert_offsets[E]
+ *      on are left as they are.  ws is not used and may be NULL.
  */
 int unipool_expert_ffn_fwd_mx8(const unipool_shape* shape, const void* x_q, const void* x_scale, const int32_t* slot_of_row,
                                const int32_t* expert_offsets, const void* w_gate_up_q, const void* w_gate_up_scale,

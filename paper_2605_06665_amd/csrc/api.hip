@@ -135,6 +135,12 @@ int32_t* extra_table(const unipool_shape& s, const WsLayout& w, void* ws) {
     if (shape->d_model > kNormMaxD)                                                                                       \
         return set_error(UNIPOOL_EINVAL, "%s: d_model=%d above %d", __func__, shape->d_model, kNormMaxD);                  \
     if (!(norm_eps >= 0.f)) return set_error(UNIPOOL_EINVAL, "%s: norm_eps must be non-negative", __func__)
+#define MX8_CHECKS()                                                                                                       \
+    if (shape->dtype != UNIPOOL_BF16)                                                                                     \
+        return set_error(UNIPOOL_EINVAL, "%s: experts in 8 bits exist in bfloat16 mode only", __func__);                   \
+    if (shape->d_model > (1 << 20) || shape->d_ff > (1 << 20))                                                            \
+        return set_error(UNIPOOL_EINVAL, "%s: d_model and d_ff must be at most 2^20 (d=%d f=%d)", __func__, shape->d_model, \
+                         shape->d_ff)
 #define NEED_WS()                                                             \
     {                                                                         \
         int rc_ = unipool::need_ws(shape, ws, ws_bytes, __func__);            \
@@ -511,7 +517,7 @@ int unipool_quantize_mx8(int dtype, long long rows, int cols, const void* src, v
     if (rows < 1 || cols < 1 || cols % 32 != 0)
         return set_error(UNIPOOL_EINVAL, "%s: rows must be positive and cols a positive multiple of 32 (rows=%lld cols=%d)", __func__,
                          rows, cols);
-    if (rows > (1LL << 40) || (rows + 63) / 64 * cdiv(cols, 128) >= (1LL << 31))
+    if (rows > (1LL << 40) || (rows + 63) / 64 * cdiv(cols, 128) >= (1LL << 24))      // 256 threads each, less than 2^32 a launch
         return set_error(UNIPOOL_EINVAL, "%s: matrix of %lld x %d is too large for one call", __func__, rows, cols);
     REQUIRE_PTR(src); REQUIRE_PTR(q); REQUIRE_PTR(scale);
     return check_hip(launch_quantize_mx8(dtype, src, rows, cols, q, scale, (hipStream_t)stream), __func__);
@@ -519,8 +525,7 @@ int unipool_quantize_mx8(int dtype, long long rows, int cols, const void* src, v
 
 int unipool_mx8_form(const unipool_shape* shape) {
     PROLOGUE();
-    if (shape->dtype != UNIPOOL_BF16)
-        return set_error(UNIPOOL_EINVAL, "%s: experts in 8 bits exist in bfloat16 mode only", __func__);
+    MX8_CHECKS();
     return mx8_ffn_form(*shape);
 }
 
@@ -529,10 +534,7 @@ int unipool_expert_ffn_fwd_mx8(const unipool_shape* shape, const void* x_q, cons
                                const void* w_down_q, const void* w_down_scale, void* h_q, void* h_scale, void* y_perm,
                                void* ws, size_t ws_bytes, void* stream) {
     PROLOGUE();
-    if (shape->dtype != UNIPOOL_BF16)
-        return set_error(UNIPOOL_EINVAL, "%s: experts in 8 bits exist in bfloat16 mode only", __func__);
-    if (shape->d_model > (1 << 20) || shape->d_ff > (1 << 20))
-        return set_error(UNIPOOL_EINVAL, "%s: d_model and d_ff must be at most 2^20 (d=%d f=%d)", __func__, shape->d_model, shape->d_ff);
+    MX8_CHECKS();
     REQUIRE_PTR(x_q); REQUIRE_PTR(x_scale); REQUIRE_PTR(expert_offsets); REQUIRE_PTR(w_gate_up_q); REQUIRE_PTR(w_gate_up_scale);
     REQUIRE_PTR(w_down_q); REQUIRE_PTR(w_down_scale); REQUIRE_PTR(h_q); REQUIRE_PTR(h_scale); REQUIRE_PTR(y_perm);
     if (!aligned(x_q, 16) || !aligned(w_gate_up_q, 16) || !aligned(w_down_q, 16) || !aligned(h_q, 16) || !aligned(y_perm, 16))

@@ -122,3 +122,13 @@ def test_binding_refuses_strided_tensors(U):
     t = torch.zeros(8, 8)[:, ::2]
     with pytest.raises(U.UniPoolError, match="contiguous"):
         U.rmsnorm(shape(U), t, None, P, 1e-6, None, P, None, None, stream=0)
+
+
+def test_limits_of_experts_and_conversion(U):
+    with pytest.raises(U.UniPoolError, match="at most 2"):
+        U.mx8_form(shape(U, T=1, E=1, k=1, d_ff=(1 << 20) + 64))
+    with pytest.raises(U.UniPoolError, match="bfloat16 mode only"):
+        U.mx8_form(shape(U, dtype=U.F32))
+    for rows, cols in ((1 << 30, 32), (1 << 26, 2048)):        # 2^24 workgroups: more threads than a launch may have
+        with pytest.raises(U.UniPoolError, match="too large"):
+            U.quantize_mx8(U.BF16, rows, cols, P, P, P, stream=0)
