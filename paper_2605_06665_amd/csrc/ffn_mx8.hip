@@ -45,10 +45,9 @@ __device__ __forceinline__ i32x8 two16(const uint4& a, const uint4& b) {
     return v;
 }
 
-// 32 columns of H of row `row`, from the sums of gate (a0, a1: 16 columns each) and up (b0, b1): the lanes l16, l16 + 16, .. of a row hold
-// 8 values each and agree on the scale of the block.  Every lane takes part; on: the row exists.
-__device__ __forceinline__ void store_h(const Mx8Args& a, const f32x4& a0, const f32x4& a1, const f32x4& b0, const f32x4& b1, bool on,
-                                        long long row, int col, int lg) {
+// 32 columns of H of a row, from the sums of gate (a0, a1: 16 columns each) and up (b0, b1): the lanes l16, l16 + 16, .. of a row hold
+// 8 values each (columns 4 lg .. and 16 + 4 lg ..) and agree on the scale of the block.  Every lane takes part.
+__device__ __forceinline__ int block_of_h(const f32x4& a0, const f32x4& a1, const f32x4& b0, const f32x4& b1, unsigned& lo, unsigned& hi) {
     float h[8];
 #pragma unroll
     for (int i = 0; i < 4; i++) {
@@ -63,13 +62,41 @@ __device__ __forceinline__ void store_h(const Mx8Args& a, const f32x4& a0, const
     const auto r32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
     m = mx8_max(__uint_as_float(r32[0]), __uint_as_float(r32[1]));
     const int byte = mx8_scale_byte(m);
+    lo = mx8_pack4(h[0], h[1], h[2], h[3], byte);
+    hi = mx8_pack4(h[4], h[5], h[6], h[7], byte);
+    return byte;
+}
+// The scale of such a block, and behind the last one what fills its word.
+__device__ __forceinline__ void store_h_scale(const Mx8Args& a, long long row, int col, int byte) {
+    unsigned char* const sc = a.h_scale + mx8_scale_at(a.S, row, col / kMxBlock);
+    *sc = (unsigned char)byte;
+    if (col + kMxBlock == a.N && a.N % kMxStep != 0) sc[1] = sc[2] = kMxBias;
+}
+// on: the row exists
+__device__ __forceinline__ void store_h(const Mx8Args& a, const f32x4& a0, const f32x4& a1, const f32x4& b0, const f32x4& b1, bool on,
+                                        long long row, int col, int lg) {
+    unsigned lo, hi;
+    const int byte = block_of_h(a0, a1, b0, b1, lo, hi);
     if (!on) return;
     unsigned char* dst = a.h + row * a.N + col + 4 * lg;
-    *reinterpret_cast<unsigned*>(dst) = mx8_pack4(h[0], h[1], h[2], h[3], byte);
-    *reinterpret_cast<unsigned*>(dst + 16) = mx8_pack4(h[4], h[5], h[6], h[7], byte);
-    unsigned char* const sc = a.h_scale + mx8_scale_at(a.S, row, col / kMxBlock);
-    if (lg == 0) *sc = (unsigned char)byte;
-    if (col + kMxBlock == a.N && a.N % kMxStep != 0 && lg == 1) *reinterpret_cast<unsigned short*>(sc + 1) = kMxBias * 0x101;      // the word's rest
+    *reinterpret_cast<unsigned*>(dst) = lo;
+    *reinterpret_cast<unsigned*>(dst + 16) = hi;
+    if (lg == 0) store_h_scale(a, row, col, byte);
+}
+
+// v[i] of group lg of 16 lanes -> v[lg] of group i
+__device__ __forceinline__ uint4 lane_groups_transposed(unsigned v0, unsigned v1, unsigned v2, unsigned v3) {
+    const auto a = __builtin_amdgcn_permlane32_swap(v0, v2, false, false), b = __builtin_amdgcn_permlane32_swap(v1, v3, false, false);
+    const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    return make_uint4(lo[0], lo[1], hi[0], hi[1]);
+}
+
+// u and v of four groups of 16 lanes -> u0 u2 v0 v2 and u1 u3 v1 v3
+__device__ __forceinline__ void pair_lane_groups(unsigned u, unsigned v, unsigned& even, unsigned& odd) {
+    const auto a = __builtin_amdgcn_permlane32_swap(u, v, false, false);
+    const auto b = __builtin_amdgcn_permlane16_swap(a[0], a[1], false, false);
+    even = b[0];
+    odd = b[1];
 }
 
 // What a reduction whose length is no multiple of 128 reads past its end.  Never written.
@@ -448,20 +475,39 @@ __global__ __launch_bounds__(2 * BN_, 2) void ffn_mx8_kernel(const Mx8Args a) {
         // acc[m][n][i] = C[row 16 (2 m + wm) + l16][weight row 16 n + 4 lg + i of the wavefront's 64]
         asm volatile("" : "+v"(ln));
         const int r16 = ln & 15, rg = ln >> 4;
+        if constexpr (GATE_UP) {
+            // two fragments at a time: their rows of 32 bytes leave in pieces of 16 a lane, half as many stores and requests as in words
 #pragma unroll
-        for (int m = 0; m < MF; m++) {
-            if (m >= mi) break;
-            const int r = (2 * m + wm) * 16 + r16;
-            const bool on = r < t.rows;
-            const long long row = t.row0 + r;
-            if constexpr (GATE_UP) {
-                store_h(a, acc[m][0], acc[m][1], acc[m][2], acc[m][3], on, row, col, rg);
-            } else {
+            for (int m = 0; m < MF; m += 2) {
+                if (m >= mi) break;
+                unsigned p[4];
+                const int byte0 = block_of_h(acc[m][0], acc[m][1], acc[m][2], acc[m][3], p[0], p[1]);
+                int byte1 = 0;
+                p[2] = p[3] = 0;
+                if (m + 1 < MF) byte1 = block_of_h(acc[m + 1][0], acc[m + 1][1], acc[m + 1][2], acc[m + 1][3], p[2], p[3]);
+                const uint4 piece = lane_groups_transposed(p[0], p[1], p[2], p[3]);
+                const int r = (2 * m + (rg & 2) + wm) * 16 + r16;
+                const long long row = t.row0 + r;
+                if (r < t.rows && (m + 1 < MF || rg < 2)) {
+                    *reinterpret_cast<uint4*>(a.h + row * a.N + col + (rg & 1) * 16) = piece;
+                    if ((rg & 1) == 0) store_h_scale(a, row, col, rg == 0 ? byte0 : byte1);
+                }
+            }
+        } else {
 #pragma unroll
-                for (int n = 0; n < 4; n++)
-                    if (on)
-                        *reinterpret_cast<uint2*>(a.y + row * a.N + col + n * 16 + 4 * rg) =
-                            pack4(acc[m][n][0], acc[m][n][1], acc[m][n][2], acc[m][n][3]);
+            for (int m = 0; m < MF; m++) {
+                if (m >= mi) break;
+                const int r = (2 * m + wm) * 16 + r16;
+                // 64 bytes of a row a store
+#pragma unroll
+                for (int n = 0; n < 4; n += 2) {
+                    const uint2 u = pack4(acc[m][n][0], acc[m][n][1], acc[m][n][2], acc[m][n][3]);
+                    const uint2 v = pack4(acc[m][n + 1][0], acc[m][n + 1][1], acc[m][n + 1][2], acc[m][n + 1][3]);
+                    uint4 piece;
+                    pair_lane_groups(u.x, v.x, piece.x, piece.z);
+                    pair_lane_groups(u.y, v.y, piece.y, piece.w);
+                    if (r < t.rows) *reinterpret_cast<uint4*>(a.y + (long long)(t.row0 + r) * a.N + col + n * 16 + 8 * rg) = piece;
+                }
             }
         }
     }
