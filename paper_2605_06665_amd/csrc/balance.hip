@@ -11,6 +11,7 @@
 // experts, k = 8, 37 sequences, softmax: counts 4.9 us, loss and gradient 19.2 us (67 MB, 3.5 TB/s).
 #include <algorithm>
 
+#include "gemm_common.h"
 #include "route_select.h"
 #include "kernels.h"
 
@@ -117,7 +118,7 @@ __device__ __forceinline__ int find_sequence(const SeqArgs& a, int t, int lane) 
 template <int GS, int VPL, bool V4, bool ONE>
 __global__ __launch_bounds__(kLossThreads) void seq_loss_kernel(const SeqArgs a) {
     constexpr int TPW = 64 / GS;
-    __shared__ float red[kLossThreads];
+    __shared__ float red[kLossThreads / 64];
     __shared__ int last, used_one;
     __shared__ int hist[ONE ? kOneCounts : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -259,10 +260,11 @@ __global__ __launch_bounds__(kLossThreads) void seq_loss_kernel(const SeqArgs a)
             }
         }
     }
-    // the workgroup's share in a fixed order; the last workgroup to hand its share in adds all of them up, in index order
+    // The workgroup's share in a fixed order; the last workgroup to hand its share in adds all of them up, in a fixed order too.  (The
+    // barriers do not wait for the gradients on their way to memory.)
     sum = wave_sum(sum);
     if (lane == 0) red[wave] = sum;
-    __syncthreads();
+    lds_barrier();
     if (threadIdx.x == 0) {
         float v = 0.f;
         for (int w = 0; w < kLossThreads / 64; w++) v += red[w];
@@ -279,20 +281,19 @@ __global__ __launch_bounds__(kLossThreads) void seq_loss_kernel(const SeqArgs a)
         last = __hip_atomic_fetch_add(&a.state[1], one, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
     }
     if constexpr (ONE) return;
-    __syncthreads();
+    lds_barrier();
     if (!last) return;
     float v = 0.f;
     for (int i = threadIdx.x; i < (int)gridDim.x; i += kLossThreads)
         v += __hip_atomic_load(&a.loss_part[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    red[threadIdx.x] = v;
-    __syncthreads();
-    for (int s = kLossThreads / 2; s > 0; s >>= 1) {
-        if (threadIdx.x < s) red[threadIdx.x] += red[threadIdx.x + s];
-        __syncthreads();
-    }
+    v = wave_sum(v);
+    if (lane == 0) red[wave] = v;                    // (thread 0 has read the shares that were there)
+    lds_barrier();
     if (threadIdx.x == 0) {
-        a.loss[0] = red[0];
-        if (a.d_sigma != nullptr) a.d_sigma[0] = a.softmax ? 0.f : red[0] / a.sigma;
+        v = 0.f;
+        for (int w = 0; w < kLossThreads / 64; w++) v += red[w];
+        a.loss[0] = v;
+        if (a.d_sigma != nullptr) a.d_sigma[0] = a.softmax ? 0.f : v / a.sigma;
     }
 }
 
