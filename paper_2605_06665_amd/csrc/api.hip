@@ -541,9 +541,10 @@ int unipool_expert_ffn_fwd_mx8(const unipool_shape* shape, const void* x_q, cons
         return set_error(UNIPOOL_EINVAL, "%s: x_q, w_gate_up_q, w_down_q, h_q and y_perm must be aligned to 16 bytes", __func__);
     if (!aligned(x_scale, 4) || !aligned(w_gate_up_scale, 16) || !aligned(w_down_scale, 16) || !aligned(h_scale, 4))
         return set_error(UNIPOOL_EINVAL, "%s: scales must be aligned to 4 bytes, those of the weights to 16", __func__);
-    (void)ws; (void)ws_bytes;
+    NEED_WS();
+    const WsLayout w = ws_layout(*shape);
     return check_hip(mx8_ffn_fwd(*shape, x_q, x_scale, slot_of_row, expert_offsets, w_gate_up_q, w_gate_up_scale, w_down_q,
-                                 w_down_scale, h_q, h_scale, y_perm, (hipStream_t)stream),
+                                 w_down_scale, h_q, h_scale, y_perm, (char*)ws + w.wpart, w.total - w.wpart, (hipStream_t)stream),
                      __func__);
 }
 

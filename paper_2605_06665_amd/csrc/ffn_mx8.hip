@@ -24,8 +24,9 @@ struct Mx8Args {
     GemmArgs g;                      // tile list only (n_tiles_n, group_m)
     const unsigned char* x;          // [rows][K], or the tokens when gather is given
     const unsigned char* x_scale;    // [ceil(K / 128)][x_rows][4]
-    long long x_rows;
-    const int32_t* gather;           // row r is row gather[r] / gather_div of x
+    long long x_rows;                // of x_scale
+    const int32_t* gather;           // row r is row gather[r] / gather_div of x, and of x_scale if scales_too
+    bool scales_too;
     int gather_div;
     const unsigned char* w;          // [E][w_rows][K]
     const unsigned char* w_scale;    // [ceil(K / 128)][E * w_rows][4]
@@ -314,7 +315,7 @@ __global__ __launch_bounds__(2 * BN_, 2) void ffn_mx8_kernel(const Mx8Args a) {
 #pragma unroll
         for (int i = 0; i < WV; i++) woff[i] = (unsigned)min(i * C::NW * 8 + r, a.N - 1 - t.nt * C::COLS) * (unsigned)a.K + at;
         wbase = reinterpret_cast<const char*>(a.w) + ((long long)t.expert * a.w_rows + t.nt * C::COLS) * a.K;
-        if (x_scales) ssrc = reinterpret_cast<const char*>(a.x_scale) + row_of(t, wave * 64 + ln, wtile) * 4;
+        if (x_scales) ssrc = reinterpret_cast<const char*>(a.x_scale) + (a.scales_too ? row_of(t, wave * 64 + ln, wtile) : (long long)t.row0 + min(wave * 64 + ln, t.rows - 1)) * 4;
         else if (w_scales) ssrc = reinterpret_cast<const char*>(a.w_scale) + (C::WS == 1 ? weight_of(t, ln * 4, 4) : weight_of(t, (wave - C::NW + C::WS) * 64 + ln, 1)) * 4;
         wnext = next_tile(wlist, a, place, BM, ln);
         if (by_lds && wnext.valid && wave < C::XS)
@@ -512,6 +513,17 @@ __global__ __launch_bounds__(2 * BN_, 2) void ffn_mx8_kernel(const Mx8Args a) {
         }
     }
     wait_vmcnt<0>();                                       // no load may land in LDS that is someone else's by then
+}
+
+// Scales of the gathered rows in group order: a tile's then lie in a few lines, where those of tokens are a line each, fetched
+// again for every tile of columns.
+__global__ __launch_bounds__(256) void gather_scales_kernel(const unsigned* __restrict__ in, long long T, const int32_t* __restrict__ gather, int gather_div,
+                                                            unsigned* __restrict__ out, long long S, int words) {
+    const long long r = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (r >= S) return;
+    const int t = gather[r] / gather_div;
+#pragma unroll 4
+    for (int w = 0; w < words; w++) out[w * S + r] = in[w * T + t];
 }
 
 template <bool GATE_UP, int BM, int BN, int NSX, int NSW> hipError_t run_tile(Mx8Args a, hipStream_t st) {
@@ -751,14 +763,21 @@ int mx8_ffn_form(const unipool_shape& s) {
 
 hipError_t mx8_ffn_fwd(const unipool_shape& s, const void* x, const void* x_scale, const int32_t* slot_of_row, const int32_t* offsets,
                        const void* wgu, const void* wgu_scale, const void* wd, const void* wd_scale, void* h, void* h_scale, void* y,
-                       hipStream_t st) {
+                       void* scratch, size_t scratch_bytes, hipStream_t st) {
     const Mx8Form form = mx8_form(s);
     const bool few = form == MX8_FEW;
     const long long S = (long long)s.T * s.k;
+    // A launch for the scales of gathered rows saves more than it takes where the tiles fetch many of their words (32768 tokens of 1536 x
+    // 4096, k = 2, 25 million words: 1590 -> 1558 us; it takes about 4).
+    const int words = cdiv(s.d_model, kMxStep);
+    const bool scales_first = slot_of_row && !few && (double)S * words * cdiv(s.d_ff, 128) >= 8e6 && (size_t)S * words * 4 <= scratch_bytes;
+    if (scales_first)
+        gather_scales_kernel<<<(unsigned)((S + 255) / 256), 256, 0, st>>>((const unsigned*)x_scale, s.T, slot_of_row, s.k, (unsigned*)scratch, S, words);
     Mx8Args a = {};
     a.offsets = offsets;
-    a.x = (const unsigned char*)x; a.x_scale = (const unsigned char*)x_scale;
-    a.x_rows = slot_of_row ? s.T : S;
+    a.x = (const unsigned char*)x; a.x_scale = (const unsigned char*)(scales_first ? scratch : x_scale);
+    a.scales_too = slot_of_row && !scales_first;
+    a.x_rows = a.scales_too ? s.T : S;
     a.gather = slot_of_row; a.gather_div = s.k;
     a.w = (const unsigned char*)wgu; a.w_scale = (const unsigned char*)wgu_scale;
     a.w_rows = 2 * s.d_ff; a.E = s.E;

@@ -121,7 +121,7 @@ int mx8_ffn_form(const unipool_shape& s);      // as unipool_mx8_form
 hipError_t launch_quantize_mx8(int dtype, const void* src, long long rows, int cols, void* q, void* scale, hipStream_t st);
 hipError_t mx8_ffn_fwd(const unipool_shape& s, const void* x, const void* x_scale, const int32_t* slot_of_row, const int32_t* offsets,
                        const void* wgu, const void* wgu_scale, const void* wd, const void* wd_scale, void* h, void* h_scale, void* y,
-                       hipStream_t st);
+                       void* scratch, size_t scratch_bytes, hipStream_t st);
 
 // ---- balance.hip -------------------------------------------------------------------
 // cnt_part and loss_part: the areas of the router's partial counts and score sums; state: two words

@@ -285,3 +285,33 @@ def test_rows_outside_the_offsets_are_left_alone(T):
     assert torch.equal(hq2[lo:hi], hq[lo:hi]) and torch.equal(hs2[:, lo:hi], hs[:, lo:hi]) and torch.equal(y2[lo:hi], y[lo:hi])
     for r in (slice(0, lo), slice(hi, None)):
         assert (hq2[r] == 0x55).all() and (hs2[:, r] == 255).all() and torch.isnan(y2[r]).all()
+
+
+@pytest.mark.parametrize("E", [16, 2])
+def test_many_gathered_rows(E):
+    """Enough of them that their scales are brought into group order first (16 experts), and the same where the workspace has no room for
+    that (2): the bits are those of rows in group order."""
+    import torch
+    U, (T, d, f, k) = lib(), (32768, 192, 8192, 2)
+    g = torch.Generator(device="cuda").manual_seed(E)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    new = lambda r, c: (torch.empty((r, c), dtype=torch.uint8, device="cuda"), torch.empty(U.mx8_scale_shape(r, c), dtype=torch.uint8, device="cuda"))  # noqa: E731
+    x, wgu, wd = new(T, d), new(E * 2 * f, d), new(E * d, f)
+    U.quantize_mx8(U.F32, T, d, rnd(T, d) * torch.exp2(torch.randint(-20, 20, (T, 1), device="cuda", generator=g)), *x)
+    U.quantize_mx8(U.F32, E * 2 * f, d, rnd(E * 2 * f, d) * 0.05, *wgu)
+    U.quantize_mx8(U.F32, E * d, f, rnd(E * d, f) * 0.05, *wd)
+    expert = torch.stack([torch.randperm(E, device="cuda", generator=g)[:k] if E > k else torch.arange(E, device="cuda") for _ in range(64)])
+    expert = expert.repeat(T // 64, 1).flatten()
+    slots = torch.argsort(expert, stable=True)
+    off = torch.searchsorted(expert[slots], torch.arange(E + 1, device="cuda")).int()
+    sh = U.Shape(T=T, d_model=d, d_ff=f, E=E, k=k, L=1, dtype=U.BF16, sigma=1.0, c=2.5, eps=1e-6, alpha_pool=0.01)
+    ws = torch.full((U.workspace_bytes(sh),), 255, dtype=torch.uint8, device="cuda")
+    tok = slots // k
+    out = []
+    for rows in ((x[0], x[1], slots.int()), (x[0][tok].contiguous(), x[1][:, tok].contiguous(), None)):
+        h, y = new(T * k, f), torch.full((T * k, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+        U.expert_ffn_fwd_mx8(sh, *rows, off, *wgu, *wd, *h, y, ws)
+        out.append((*h, y))
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
+    assert torch.isfinite(out[0][2]).all()
