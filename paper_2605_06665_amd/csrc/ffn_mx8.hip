@@ -767,10 +767,11 @@ hipError_t mx8_ffn_fwd(const unipool_shape& s, const void* x, const void* x_scal
     const Mx8Form form = mx8_form(s);
     const bool few = form == MX8_FEW;
     const long long S = (long long)s.T * s.k;
-    // A launch for the scales of gathered rows saves more than it takes where the tiles fetch many of their words (32768 tokens of 1536 x
-    // 4096, k = 2, 25 million words: 1590 -> 1558 us; it takes about 4).
-    const int words = cdiv(s.d_model, kMxStep);
-    const bool scales_first = slot_of_row && !few && (double)S * words * cdiv(s.d_ff, 128) >= 8e6 && (size_t)S * words * 4 <= scratch_bytes;
+    // A launch for the scales of gathered rows (4 us) where every one would be fetched for 32 tiles of columns or more, 3 million words and
+    // over in all (192 experts of 1536 x 4096, k = 2, 4001 tokens 734 -> 726 us, 8192 787 -> 773, 32768 1570 -> 1548; but 64 experts of
+    // 768 x 2048, k = 8, 16384 tokens, 16 tiles of columns, 809 / 809, and 512 of 1024 x 704, k = 8, 16384 tokens 568 / 576).
+    const int words = cdiv(s.d_model, kMxStep), tiles = cdiv(s.d_ff, 128);
+    const bool scales_first = slot_of_row && !few && tiles >= 32 && (double)S * words * tiles >= 3e6 && (size_t)S * words * 4 <= scratch_bytes;
     if (scales_first)
         gather_scales_kernel<<<(unsigned)((S + 255) / 256), 256, 0, st>>>((const unsigned*)x_scale, s.T, slot_of_row, s.k, (unsigned*)scratch, S, words);
     Mx8Args a = {};
