@@ -547,10 +547,10 @@ template <bool GATE_UP, int BM, int BN, int NSX, int NSW> hipError_t run_tile(Mx
 //     tokens of 90 experts of 832 x 1472, k = 3 29.1 / 24.9), or where the reductions are long (192 experts of 1536 x 4096, k = 2, 4 tokens 44 / 52,
 //     64 tokens 344 / 359; but 40 tokens of the 90 experts 76 / 68);
 //   128 weight rows, two workgroups to a compute unit, while there are less than 16 rounds of the wide ones, or 4 with more than 96
-//     rows (64 x 128 / 96 x 128 / 64 x 256 / 128 x 256: 90 experts, 50 rows, hot 106 / 110 / 117 / 114; 16 experts of 768 x 2048, 37 rows 28.5 /
-//     29.2 / 31.8 / 35.8, 187 rows 50 / 45 / 51 / 47);
-//   256 weight rows beyond (192 experts of 1536 x 4096, 11 rows 719 / 726 / 651 / 670, 42 rows 761 / 759 / 717 / 728, 85 rows 1087 / 913 / 1004 / 789);
-//   192 rows where experts take several tiles of 128 (the 192 experts, 125 rows: 128 x 256 961, 192 x 256 866; 512 of 1024 x 704, 256 rows 574 / 560).
+//     rows (64 x 128 / 96 x 128 / 64 x 256 / 128 x 256: 90 experts, 50 rows, hot 108 / 106 / 115 / 112; 16 experts of 768 x 2048, 37 rows 28.0 /
+//     29.2 / 31.3 / 35.4, 187 rows 49 / 44 / 50 / 46);
+//   256 weight rows beyond (192 experts of 1536 x 4096, 11 rows 716 / 729 / 653 / 691, 42 rows 759 / 760 / 712 / 734, 85 rows 1087 / 906 / 1007 / 789);
+//   192 rows where experts take several tiles of 128 (the 192 experts, 125 rows: 128 x 256 939, 192 x 256 869; 512 of 1024 x 704, 256 rows 582 / 567).
 enum Mx8Form { MX8_FEW, MX8_64x128, MX8_96x128, MX8_64x256, MX8_128x256, MX8_192x256 };
 Mx8Form mx8_form(const unipool_shape& s) {
     const double S = (double)s.T * s.k, used = s.E * -std::expm1(-S / s.E), r = S / used, most = r + 2.0 * std::sqrt(r);
