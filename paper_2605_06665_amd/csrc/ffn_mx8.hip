@@ -767,7 +767,7 @@ hipError_t mx8_ffn_fwd(const unipool_shape& s, const void* x, const void* x_scal
     const Mx8Form form = mx8_form(s);
     const bool few = form == MX8_FEW;
     const long long S = (long long)s.T * s.k;
-    // A launch for the scales of gathered rows (4 us) where every one would be fetched for 32 tiles of columns or more, 3 million words and
+    // A launch for the scales of gathered rows (4 to 6 us) where every one would be fetched for 32 tiles of columns or more, 3 million words and
     // over in all (192 experts of 1536 x 4096, k = 2, 4001 tokens 734 -> 726 us, 8192 787 -> 773, 32768 1570 -> 1548; but 64 experts of
     // 768 x 2048, k = 8, 16384 tokens, 16 tiles of columns, 809 / 809, and 512 of 1024 x 704, k = 8, 16384 tokens 568 / 576).
     const int words = cdiv(s.d_model, kMxStep), tiles = cdiv(s.d_ff, 128);
