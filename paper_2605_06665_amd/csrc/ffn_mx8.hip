@@ -485,11 +485,12 @@ __global__ __launch_bounds__(2 * BN_, 2) void ffn_mx8_kernel(const Mx8Args a) {
                 const int byte0 = block_of_h(acc[m][0], acc[m][1], acc[m][2], acc[m][3], p[0], p[1]);
                 int byte1 = 0;
                 p[2] = p[3] = 0;
-                if (m + 1 < MF) byte1 = block_of_h(acc[m + 1][0], acc[m + 1][1], acc[m + 1][2], acc[m + 1][3], p[2], p[3]);
+                const int m1 = m + 1 < MF ? m + 1 : m;
+                if (m + 1 < mi) byte1 = block_of_h(acc[m1][0], acc[m1][1], acc[m1][2], acc[m1][3], p[2], p[3]);
                 const uint4 piece = lane_groups_transposed(p[0], p[1], p[2], p[3]);
                 const int r = (2 * m + (rg & 2) + wm) * 16 + r16;
                 const long long row = t.row0 + r;
-                if (r < t.rows && (m + 1 < MF || rg < 2)) {
+                if (r < t.rows && (m + 1 < mi || rg < 2)) {
                     *reinterpret_cast<uint4*>(a.h + row * a.N + col + (rg & 1) * 16) = piece;
                     if ((rg & 1) == 0) store_h_scale(a, row, col, rg == 0 ? byte0 : byte1);
                 }
