@@ -62,6 +62,4 @@ __device__ __forceinline__ size_t mx8_scale_at(size_t rows, size_t row, int b) {
 
 }  // namespace
 
-constexpr int kMx8Rows = 64;       // rows of a workgroup of the conversion
-
 }  // namespace unipool
