@@ -49,12 +49,14 @@ __device__ __forceinline__ i32x8 two16(const uint4& a, const uint4& b) {
 // 32 columns of H of a row, from the sums of gate (a0, a1: 16 columns each) and up (b0, b1): the lanes l16, l16 + 16, .. of a row hold
 // 8 values each (columns 4 lg .. and 16 + 4 lg ..) and agree on the scale of the block.  Every lane takes part.
 __device__ __forceinline__ int block_of_h(const f32x4& a0, const f32x4& a1, const f32x4& b0, const f32x4& b1, unsigned& lo, unsigned& hi) {
-    float h[8];
+    // silu(a) b step by step for all values, so that no instruction waits for the exponential or the reciprocal in front of it
+    float h[8], p[8];
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        h[i] = silu_f(a0[i]) * b0[i];
-        h[4 + i] = silu_f(a1[i]) * b1[i];
-    }
+    for (int i = 0; i < 8; i++) p[i] = __expf(-(i < 4 ? a0[i] : a1[i - 4]));
+#pragma unroll
+    for (int i = 0; i < 8; i++) p[i] = __builtin_amdgcn_rcpf(1.0f + p[i]);
+#pragma unroll
+    for (int i = 0; i < 8; i++) h[i] = (i < 4 ? a0[i] : a1[i - 4]) * p[i] * (i < 4 ? b0[i] : b1[i - 4]);
     float m = h[0];
 #pragma unroll
     for (int i = 1; i < 8; i++) m = mx8_max(m, h[i]);

@@ -44,16 +44,15 @@ __device__ __forceinline__ int mx8_scale_byte(float amax) {
     const int e = (int)(b >> 23) - 135 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
     return max(e, -127) + kMxBias;
 }
-// 2^-e, exact: e lies between -127 and 120
-__device__ __forceinline__ float mx8_inverse(int byte) { return __uint_as_float((unsigned)(254 - byte) << 23); }
-
-// Four values to four e4m3 bytes, the first lowest.  |v| <= 448 after the scale, so the conversion never overflows.
+// Four values to four e4m3 bytes, the first lowest.  The instruction divides by the power of two whose exponent bits it is given, and
+// |v| <= 448 after that, so it never overflows.
 __device__ __forceinline__ unsigned mx8_pack4(float a, float b, float c, float d, int byte) {
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
     if (byte == kMxNan) return 0x7f7f7f7fu;
-    const float s = mx8_inverse(byte);
-    int r = __builtin_amdgcn_cvt_pk_fp8_f32(a * s, b * s, 0, false);
-    r = __builtin_amdgcn_cvt_pk_fp8_f32(c * s, d * s, r, true);
-    return (unsigned)r;
+    const float scale = __uint_as_float((unsigned)byte << 23);
+    s16x2 r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(s16x2{0, 0}, a, b, scale, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, c, d, scale, true);
+    return __builtin_bit_cast(unsigned, r);
 }
 __device__ __forceinline__ unsigned char mx8_pack1(float a, int byte) { return (unsigned char)(mx8_pack4(a, a, a, a, byte) & 0xffu); }
 
