@@ -68,18 +68,13 @@ def test_balance_loss(U):
 
 def test_router_backward_with_further_gradients(U):
     sh = shape(U)
-    for i in range(9):
-        if i in (5, 6):
-            continue
-        args = [P] * 9
-        args[i if i < 5 else i] = None
-        if i < 5 or i >= 7:
-            a = dict(zip(("x", "w", "z", "idx", "dgate"), args[:5]))
-            with pytest.raises(U.UniPoolError, match="NULL"):
-                U.route_bwd_add(sh, a["x"], a["w"], a["z"], a["idx"], a["dgate"], None, None, None, args[7], args[8], P if i != 8 else None,
-                                False, ws(U, sh), stream=0)
+    names = ("x", "w_router", "logits", "topk_idx", "dgate", "aux_coef", "d_logits", "d_sigma_in", "d_w_router", "d_sigma", "dx")
+    for n in names:
+        if n not in ("aux_coef", "d_logits", "d_sigma_in"):
+            with pytest.raises(U.UniPoolError, match="%s is NULL" % n):
+                U.route_bwd_add(sh, *[None if m == n else P for m in names], False, ws(U, sh), stream=0)
     with pytest.raises(U.UniPoolError, match="workspace"):
-        U.route_bwd_add(sh, P, P, P, P, P, None, None, None, P, P, P, False, None, stream=0)
+        U.route_bwd_add(sh, *[P] * len(names), False, None, stream=0)
 
 
 def test_quantize(U):
@@ -115,6 +110,9 @@ def test_experts(U):
     big = shape(U, T=1, E=1, k=1, d_ff=(1 << 20) + 64)
     with pytest.raises(U.UniPoolError, match="at most 2"):
         call(sh=big, ws=ws(U, big))
+    for w, msg in ((None, "workspace is NULL"), (Ws(64), "64 bytes")):
+        with pytest.raises(U.UniPoolError, match=msg):
+            call(ws=w)
 
 
 def test_binding_refuses_strided_tensors(U):
