@@ -553,9 +553,10 @@ template <bool GATE_UP, int BM, int BN, int NSX, int NSW> hipError_t run_tile(Mx
 
 // Which form a call takes, from the rows r of an expert that has any (as if the picks were independent) and from how many rounds its
 // gate-up tiles of 128 rows by 256 weight rows are on the card's compute units.  All of the call, us, three sets of weights in turn:
-//   few: up to 64 tokens, with few tasks (64 experts of 768 x 2048, k = 2, 1 token: few 16.9, tiles of 64 x 128 22.2, 4 tokens 20.6 / 23.5; but 5
-//     tokens of 90 experts of 832 x 1472, k = 3 29.1 / 24.9), or where the reductions are long (192 experts of 1536 x 4096, k = 2, 4 tokens 44 / 52,
-//     64 tokens 344 / 359; but 40 tokens of the 90 experts 76 / 68);
+//   few: up to 64 tokens, with few tasks (64 experts of 768 x 2048, k = 2, 1 token: few 14.5, tiles of 64 x 128 21.8, 4 tokens 18.6 / 23.4; but 5
+//     tokens of 90 experts of 832 x 1472, k = 3 25.0 / 25.0, 40 tokens 77 / 68), or where the reductions are long (192 experts of 1536 x
+//     4096, k = 2, 4 tokens 41 / 52, 64 tokens 342 / 358; up to three rows an expert also the 64 experts, 16 tokens 38 / 41, 32 tokens
+//     50 / 53, but 16 experts of 768 x 2048, 64 tokens, k = 1 29.4 / 27.2);
 //   128 weight rows, two workgroups to a compute unit, while there are less than 16 rounds of the wide ones, or 4 with more than 96
 //     rows (64 x 128 / 96 x 128 / 64 x 256 / 128 x 256: 90 experts, 50 rows, hot 108 / 106 / 115 / 112; 16 experts of 768 x 2048, 37 rows 28.0 /
 //     29.2 / 31.3 / 35.4, 187 rows 49 / 44 / 50 / 46);
@@ -567,7 +568,8 @@ Mx8Form mx8_form(const unipool_shape& s) {
     const int cus = num_cus();
     if (s.T <= 16 || (s.T <= 64 && S <= 8.0 * s.E)) {
         const double tasks = std::min(S, (double)s.E) * (s.d_ff / 32);
-        if (tasks <= 2.0 * cus || std::min(s.d_model, s.d_ff) >= 1536) return MX8_FEW;
+        const int least = std::min(s.d_model, s.d_ff);
+        if (tasks <= 2.0 * cus || least >= 1536 || (least >= 768 && s.d_ff >= 2048 && S <= 3.0 * s.E)) return MX8_FEW;
     }
     const double rounds = used * std::ceil((r + std::sqrt(r)) / 128) * cdiv(s.d_ff, 128) / cus;
     if (r > 96) return rounds < 4 ? MX8_96x128 : most <= 128 ? MX8_128x256 : MX8_192x256;
@@ -589,8 +591,8 @@ template <bool GATE_UP> hipError_t run_mx8(Mx8Form form, const Mx8Args& a, hipSt
 // Few rows per expert (decoding, short prompts): one pass over the weights of the experts that have rows, bound by the bytes that are
 // in flight.  A wavefront owns 16 NF weight rows of one expert (gate-up: 32 gate rows and the 32 up rows they meet, which are a whole
 // block of H) for all rows of the expert; weights go from memory to registers, whole 128-byte lines at a time (few_rows.h), D
-// steps of 128 indices ahead, with no LDS and no barrier.  192 experts of 1536 x 4096, 4 tokens: 21.8 us for 104 MB (4.8 TB/s), 16 us for
-// 52 MB (at the rate of a large copy 20.5 and 10.3).
+// steps of 128 indices ahead, with no LDS and no barrier.  192 experts of 1536 x 4096, 4 tokens: 20.1 us for 104 MB (5.2 TB/s), 13.4 us
+// for 52 MB (at the rate of a large copy 20.5 and 10.3; the weights lie in the last-level cache here, else 40.4 for both).
 // ---------------------------------------------------------------------------------------------
 template <typename V> __device__ __forceinline__ i32x8 two16(const V& a, const V& b) {
     union { V v[2]; i32x8 i; } u;
@@ -751,9 +753,11 @@ template <bool GATE_UP> hipError_t run_few_mx8(const unipool_shape& s, const Mx8
     const int S = s.T * s.k, cus = num_cus();
     const int most = std::min(S, s.E) * (a.N / (GATE_UP ? 32 : 16));        // tasks if every row had an expert of its own
     const bool one = s.T <= 16;                            // an expert gets a token at most once
-    // At most one wavefront per SIMD: all its registers hold steps in flight.
+    // At most one wavefront per SIMD.  More steps in flight than these would fit its registers, but every step is code of its own that has to
+    // come from memory too (6 and 16 steps: 192 experts of 1536 x 4096, k = 2, 1 token 22.6 us instead of 19.9, 4 tokens 44.0 instead of 40.4; 32
+    // of 512 x 512, 8 tokens 17.5 instead of 14.4; 4 and 12 steps: 21.8, 42.7, 15.1; 3 and 4: 21.2, 40.3, 13.1).
     if (most <= 4 * cus) {
-        constexpr int D1 = GATE_UP ? 6 : 16, DM = GATE_UP ? 5 : 8;
+        constexpr int D1 = GATE_UP ? 3 : 8, DM = GATE_UP ? 2 : 4;
         if (one) few_mx8_kernel<GATE_UP, NF, 1, 1, D1, D1><<<most, 64, 0, st>>>(a);
         else few_mx8_kernel<GATE_UP, NF, 1, 2, D1, DM><<<most, 64, 0, st>>>(a);
         return hipGetLastError();
