@@ -100,6 +100,7 @@ __device__ __forceinline__ int few_experts(const int32_t* offsets, int E, int* l
     }
 #pragma unroll
     for (int p = 0; p < kMaxE / kThreads; p++) {
+        if (p * kThreads >= E) break;
         const int e = p * kThreads + tid, r0 = first[p], n = rows[p];
         const unsigned long long has = __ballot(n > 0);
         if (lane == 0) wcnt[p][wave] = __popcll(has);
