@@ -368,7 +368,7 @@ int unipool_quantize_mx8(int dtype, long long rows, int cols, const void* src, v
  *      rows [S, d] in group order when it is NULL;  expert_offsets [E+1];  w_gate_up_q [E, 2 d_ff, d], w_down_q [E, d, d_ff] with
  *      their scales.  The values, the weights' scales and y_perm must be aligned to 16 bytes, the other scales to 4; d, d_ff <= 2^20.
  * out: h_q [S, d_ff], h_scale (H in MX8);  y_perm [S, d] bfloat16.  Rows in front of expert_offsets[0] and from expert_offsets[E]
- *      on are left as they are.
+ *      on are left as they are, and their entries of slot_of_row are not read.
  */
 int unipool_expert_ffn_fwd_mx8(const unipool_shape* shape, const void* x_q, const void* x_scale, const int32_t* slot_of_row,
                                const int32_t* expert_offsets, const void* w_gate_up_q, const void* w_gate_up_scale,

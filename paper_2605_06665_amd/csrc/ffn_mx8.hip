@@ -526,11 +526,11 @@ __global__ __launch_bounds__(2 * BN_, 2) void ffn_mx8_kernel(const Mx8Args a) {
 }
 
 // Scales of the gathered rows in group order: a tile's then lie in a few lines, where those of tokens are a line each, fetched
-// again for every tile of columns.
+// again for every tile of columns.  Rows outside the offsets have no token: their entries of gather may hold anything and are not read.
 __global__ __launch_bounds__(256) void gather_scales_kernel(const unsigned* __restrict__ in, long long T, const int32_t* __restrict__ gather, int gather_div,
-                                                            unsigned* __restrict__ out, long long S, int words) {
+                                                            const int32_t* __restrict__ offsets, int E, unsigned* __restrict__ out, long long S, int words) {
     const long long r = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (r >= S) return;
+    if (r >= S || r < offsets[0] || r >= offsets[E]) return;
     const int t = gather[r] / gather_div;
 #pragma unroll 4
     for (int w = 0; w < words; w++) out[w * S + r] = in[w * T + t];
@@ -788,7 +788,8 @@ hipError_t mx8_ffn_fwd(const unipool_shape& s, const void* x, const void* x_scal
     const int words = cdiv(s.d_model, kMxStep), tiles = cdiv(s.d_ff, 128);
     const bool scales_first = slot_of_row && !few && tiles >= 32 && (double)S * words * tiles >= 3e6 && (size_t)S * words * 4 <= scratch_bytes;
     if (scales_first)
-        gather_scales_kernel<<<(unsigned)((S + 255) / 256), 256, 0, st>>>((const unsigned*)x_scale, s.T, slot_of_row, s.k, (unsigned*)scratch, S, words);
+        gather_scales_kernel<<<(unsigned)((S + 255) / 256), 256, 0, st>>>((const unsigned*)x_scale, s.T, slot_of_row, s.k, offsets, s.E,
+                                                                          (unsigned*)scratch, S, words);
     Mx8Args a = {};
     a.offsets = offsets;
     a.x = (const unsigned char*)x; a.x_scale = (const unsigned char*)(scales_first ? scratch : x_scale);
