@@ -316,7 +316,8 @@ int unipool_pool_aux_loss(const unipool_shape* shape, const int32_t* counts, con
  *   d_logits[t, i] = d loss / d logits[t, i],  d_sigma = d loss / d sigma   (f is constant for differentiation; softmax: d_sigma = 0)
  * Sequences may be empty: their counts are zero and they add nothing.  Tokens outside all sequences (padding in front of the first or
  * behind the last) are not read into any sum, and their rows of d_logits are zero.  seq_offsets must not decrease; what lies
- * outside [0, T] is cut off.
+ * outside [0, T] is cut off.  NORM: a token whose logits are all zero (or their squares, in float) adds nothing to loss and
+ * gradients, also with eps = 0.
  * in : seq_offsets [n_seq + 1] int32 (device), 1 <= n_seq <= 2^20;  logits [T, E] float and topk_idx [T, k] from unipool_route.
  * out: counts [n_seq, E] int32;  loss [1] float;  d_logits [T, E] float or NULL;  d_sigma [1] float or NULL.
  */

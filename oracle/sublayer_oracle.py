@@ -54,10 +54,10 @@ def seq_balance_loss(logits, topk_idx, offsets, alpha, router, sigma, c, eps):
                 dz[t] = p * (coef - coef @ p)
             else:
                 n = np.sqrt(z[t] @ z[t])
-                s = sigma * c * np.maximum(z[t], 0.0) / (n + eps)
-                loss += coef @ s
-                d_sigma += coef @ s / sigma
-                if n > 0:
+                if n > 0:                               # logits that are all zero have no direction: nothing, also with eps = 0
+                    s = sigma * c * np.maximum(z[t], 0.0) / (n + eps)
+                    loss += coef @ s
+                    d_sigma += coef @ s / sigma
                     gz = np.where(z[t] > 0, coef * sigma * c, 0.0)
                     dz[t] = gz / (n + eps) - z[t] * (gz @ z[t]) / (n * (n + eps) ** 2)
     return counts, loss, dz, d_sigma

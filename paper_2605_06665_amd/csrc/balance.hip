@@ -241,7 +241,7 @@ __global__ __launch_bounds__(kLossThreads) void seq_loss_kernel(const SeqArgs a)
                 dot += dz[i] * z[i];
             }
             dot = group_reduce_f<GS>(dot, add);
-            part = dot * inv;                                          // <coef, s>
+            part = n > 0.f ? dot * inv : 0.f;                          // <coef, s>; a token without a direction has none (eps may be 0)
             const float back = n > 0.f ? dot * inv * inv / n : 0.f;
 #pragma unroll
             for (int i = 0; i < VPL; i++) dz[i] = n > 0.f ? dz[i] * inv - z[i] * back : 0.f;

@@ -183,3 +183,39 @@ def test_many_empty_sequences_between_those_with_tokens(router):
     z = np.random.default_rng(12).standard_normal((T, E)).astype(np.float32)
     off = [0] * 700 + [1, 2, 2, 3] + [7] * 1500 + [100] * 3 + [101, 150] + [151] * 900 + [300] * 2
     check(T, E, k, router, z, off, run(T, E, k, router, z, picks(z, k), off))
+
+
+@pytest.mark.parametrize("T,E", [(20, 8), (400, 70)])
+@pytest.mark.parametrize("tiny", [0.0, 1e-30])
+def test_tokens_without_a_direction_and_without_eps(T, E, tiny, monkeypatch):
+    """Logits that are all zero, or so small that their squares are: no part of loss and gradients, where 1 / norm is infinite.  The
+    router's backward pass takes the gradients of a batch with zero logits in."""
+    import sys
+
+    import torch
+    monkeypatch.setattr(sys.modules[__name__], "EPS", 0.0)
+    k = 2
+    z = np.random.default_rng(T).standard_normal((T, E)).astype(np.float32)
+    z[3], z[T - 1] = 0.0, tiny
+    off = [0, T // 2, T]
+    got = run(T, E, k, "norm", z, picks(z, k), off)
+    zr = np.where(np.abs(z) < 1e-20, 0.0, z)                       # what the squares in float make of them
+    c_ref, l_ref, dz_ref, ds_ref = O.seq_balance_loss(zr, picks(z, k), off, ALPHA, "norm", SIGMA, CC, EPS)
+    assert np.array_equal(host(got[0]), c_ref)
+    assert abs(host(got[1])[0] - l_ref) <= C * abs(l_ref) and abs(host(got[3])[0] - ds_ref) <= C * abs(ds_ref)
+    assert np.isfinite(host(got[2])).all() and not host(got[2])[[3, T - 1]].any()
+    if tiny:                                                       # (its score itself is infinite: relu(z) / 0)
+        return
+    U, d = lib(), 64
+    sh = shape(T, E, k, "norm", d)
+    ws = torch.empty(U.workspace_bytes(sh), dtype=torch.uint8, device="cuda")
+    x, w, dgate = torch.randn(T, d, device="cuda"), torch.randn(E, d, device="cuda"), torch.ones(T, k, device="cuda")
+    out = []
+    for extra in ((None, None), (got[2], got[3])):
+        dw, ds, dx = torch.zeros(E, d, device="cuda"), torch.zeros(1, device="cuda"), torch.zeros(T, d, device="cuda")
+        U.route_bwd_add(sh, x, w, dev(z), dev(picks(z, k)), dgate, None, *extra, dw, ds, dx, False, ws)
+        out.append((dw, ds, dx))
+    assert all(torch.isfinite(t).all() for o in out for t in o)
+    # sigma's own gradient is a sum of k T terms, the scores over sigma
+    scores = float(host(out[0][1])[0])
+    assert abs(float(host(out[1][1])[0]) - scores - ds_ref) <= C * (abs(scores) + CC * k * T + abs(ds_ref))

@@ -95,3 +95,12 @@ def test_mx8_scales_and_blocks():
     assert s.shape == (2, 6, 4) and (s[1, :, 1:] == 127).all()
     e = np.repeat(np.transpose(s, (1, 0, 2)).reshape(6, -1)[:, :5].astype(int) - 127, 32, axis=1)
     assert (np.abs(O.from_mx8(q, s) - w) <= np.maximum(np.abs(w) * 2.0 ** -4, 2.0 ** (e - 10.0))).all()
+
+
+def test_balance_of_a_token_without_a_direction():
+    z = np.array([[1.0, 2.0], [0.0, 0.0], [-1.0, 3.0]])
+    idx = np.array([[1], [0], [1]])
+    counts, loss, dz, ds = O.seq_balance_loss(z, idx, [0, 3], 0.3, "norm", 2.0, 1.5, 0.0)
+    near = O.seq_balance_loss(z, idx, [0, 3], 0.3, "norm", 2.0, 1.5, 1e-12)
+    assert np.array_equal(counts, [[1, 2]]) and not dz[1].any() and np.isfinite(loss)
+    assert abs(loss - near[1]) < 1e-11 and abs(ds - near[3]) < 1e-11 and np.abs(dz - near[2]).max() < 1e-11
