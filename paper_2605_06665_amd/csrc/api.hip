@@ -517,7 +517,8 @@ int unipool_quantize_mx8(int dtype, long long rows, int cols, const void* src, v
     if (rows < 1 || cols < 1 || cols % 32 != 0)
         return set_error(UNIPOOL_EINVAL, "%s: rows must be positive and cols a positive multiple of 32 (rows=%lld cols=%d)", __func__,
                          rows, cols);
-    if (rows > (1LL << 40) || (rows + 63) / 64 * cdiv(cols, 128) >= (1LL << 24))      // 256 threads each, less than 2^32 a launch
+    // 256 threads each, less than 2^32 a launch; both factors in 64 bits, which cols + 127 may need
+    if (rows > (1LL << 40) || (rows + 63) / 64 * ((cols + 127LL) / 128) >= (1LL << 24))
         return set_error(UNIPOOL_EINVAL, "%s: matrix of %lld x %d is too large for one call", __func__, rows, cols);
     REQUIRE_PTR(src); REQUIRE_PTR(q); REQUIRE_PTR(scale);
     return check_hip(launch_quantize_mx8(dtype, src, rows, cols, q, scale, (hipStream_t)stream), __func__);

@@ -130,3 +130,9 @@ def test_limits_of_experts_and_conversion(U):
     for rows, cols in ((1 << 30, 32), (1 << 26, 2048)):        # 2^24 workgroups: more threads than a launch may have
         with pytest.raises(U.UniPoolError, match="too large"):
             U.quantize_mx8(U.BF16, rows, cols, P, P, P, stream=0)
+
+
+def test_conversion_of_the_longest_rows(U):
+    for cols in (2147483520 + 32, 2147483616):                 # 2^24 workgroups a row of 64, where cols + 127 passes 31 bits
+        with pytest.raises(U.UniPoolError, match="too large"):
+            U.quantize_mx8(U.BF16, 1, cols, P, P, P, stream=0)
