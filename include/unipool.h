@@ -318,7 +318,7 @@ int unipool_pool_aux_loss(const unipool_shape* shape, const int32_t* counts, con
  * behind the last) are not read into any sum, and their rows of d_logits are zero.  seq_offsets must not decrease; what lies
  * outside [0, T] is cut off.  NORM: a token whose logits are all zero (or their squares, in float) adds nothing to loss and
  * gradients, also with eps = 0.
- * in : seq_offsets [n_seq + 1] int32 (device), 1 <= n_seq <= 2^20;  logits [T, E] float and topk_idx [T, k] from unipool_route.
+ * in : seq_offsets [n_seq + 1] int32 (device), 1 <= n_seq <= 2^20;  T <= 2^31 - 64;  logits [T, E] float and topk_idx [T, k] from unipool_route.
  * out: counts [n_seq, E] int32;  loss [1] float;  d_logits [T, E] float or NULL;  d_sigma [1] float or NULL.
  */
 int unipool_seq_balance_loss(const unipool_shape* shape, int n_seq, const int32_t* seq_offsets, float alpha_seq,

@@ -502,6 +502,8 @@ int unipool_seq_balance_loss(const unipool_shape* shape, int n_seq, const int32_
     PROLOGUE();
     if (n_seq < 1 || n_seq > (1 << 20))
         return set_error(UNIPOOL_EINVAL, "%s: n_seq=%d outside [1, 2^20]", __func__, n_seq);
+    if (shape->T > INT32_MAX - 63)      // a token's number plus those of a round stays below 2^31
+        return set_error(UNIPOOL_EINVAL, "%s: T=%d above 2^31 - 64", __func__, shape->T);
     REQUIRE_PTR(seq_offsets); REQUIRE_PTR(logits); REQUIRE_PTR(topk_idx); REQUIRE_PTR(counts); REQUIRE_PTR(loss);
     NEED_WS();
     const WsLayout w = ws_layout(*shape);

@@ -307,11 +307,14 @@ hipError_t launch_seq_balance_loss(const unipool_shape& s, int n_seq, const int3
     a.offsets = seq_offsets; a.logits = logits; a.topk_idx = topk_idx; a.counts = counts; a.part = cnt_part; a.state = state;
     a.loss_part = loss_part; a.loss = loss; a.d_logits = d_logits; a.d_sigma = d_sigma;
     a.T = s.T; a.E = s.E; a.k = s.k; a.n_seq = n_seq;
+    // In 64 bits: T, n_seq kTokensPerPart and a workgroup's tokens are each below 2^31, their sums are not.
     // (parts n_seq <= T / kTokensPerPart + n_seq <= 2 T / kTokensPerPart: fits the area of the partial counts, T / 64 rows)
-    a.parts = (long long)n_seq * kTokensPerPart <= s.T ? std::min(cdiv(s.T, n_seq * kTokensPerPart), 1024) : 1;
+    const auto pieces = [](long long n, long long of) { return (n + of - 1) / of; };
+    const long long per_part = (long long)n_seq * kTokensPerPart;
+    a.parts = per_part <= s.T ? (int)std::min(pieces(s.T, per_part), 1024LL) : 1;
     a.alpha = alpha; a.sigma = s.sigma; a.c = s.c; a.eps = s.eps;
     a.softmax = s.router == UNIPOOL_ROUTER_SOFTMAX;
-    a.tok_per_block = kLossTokens * cdiv(cdiv(s.T, kLossTokens), kLossBlocks);      // (a word per 64 tokens at most in loss_part)
+    a.tok_per_block = (int)(kLossTokens * pieces(pieces(s.T, kLossTokens), kLossBlocks));      // (a word per 64 tokens at most in loss_part)
     // A few tokens go in one launch instead of two (128 tokens, 8 experts 8.1 -> 5.2 us on the device)
     const bool one = s.T <= kOneTokens && (long long)n_seq * s.E <= kOneCounts;
     if (one) {
@@ -321,7 +324,7 @@ hipError_t launch_seq_balance_loss(const unipool_shape& s, int n_seq, const int3
         if (a.parts > 1) seq_count_sum_kernel<<<(unsigned)(((size_t)n_seq * s.E + 255) / 256), 256, 0, st>>>(a);
     }
     const bool v4 = s.E % 4 == 0 && (((uintptr_t)logits | (uintptr_t)d_logits) & 15) == 0;
-    const int grid = cdiv(s.T, a.tok_per_block);
+    const int grid = (int)pieces(s.T, a.tok_per_block);
     auto run = [&](auto gs, auto vpl) {
         if (one && v4) seq_loss_kernel<gs(), vpl(), true, true><<<1, kLossThreads, 0, st>>>(a);
         else if (one) seq_loss_kernel<gs(), vpl(), false, true><<<1, kLossThreads, 0, st>>>(a);

@@ -219,3 +219,22 @@ def test_tokens_without_a_direction_and_without_eps(T, E, tiny, monkeypatch):
     # sigma's own gradient is a sum of k T terms, the scores over sigma
     scores = float(host(out[0][1])[0])
     assert abs(float(host(out[1][1])[0]) - scores - ds_ref) <= C * (abs(scores) + CC * k * T + abs(ds_ref))
+
+
+def test_counts_of_many_sequences_in_parts_past_30_bits_of_tokens():
+    """Tokens and the tokens that a round of workgroups counts pass 2^31 together.  One expert with one pick a token: counts are the lengths,
+    every score is 1, the loss alpha."""
+    import torch
+    U, T, n_seq = lib(), 1_200_000_000, 250_000
+    sh = shape(T, 1, 1, "softmax")
+    z, idx = torch.zeros((T, 1), device="cuda"), torch.zeros((T, 1), dtype=torch.int32, device="cuda")
+    off = torch.arange(n_seq + 1, device="cuda").mul_(4800).int()
+    off[-1] = T
+    off[1:-1] += torch.randint(-2000, 2000, (n_seq - 1,), device="cuda").int()
+    ws = torch.empty(U.workspace_bytes(sh), dtype=torch.uint8, device="cuda")
+    counts, loss = torch.full((n_seq, 1), -1, dtype=torch.int32, device="cuda"), torch.full((1,), float("nan"), device="cuda")
+    U.seq_balance_loss(sh, n_seq, off, ALPHA, z, idx, counts, loss, None, None, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(counts[:, 0], off[1:] - off[:-1])
+    # a wavefront adds the shares of its tokens one after the other, 16 lanes' groups of them; then 16 wavefronts and 512 workgroups
+    assert abs(float(loss) - ALPHA) <= (T / (512 * 16 * 4) + 64) * 2.0 ** -24 * ALPHA

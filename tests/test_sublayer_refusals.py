@@ -136,3 +136,9 @@ def test_conversion_of_the_longest_rows(U):
     for cols in (2147483520 + 32, 2147483616):                 # 2^24 workgroups a row of 64, where cols + 127 passes 31 bits
         with pytest.raises(U.UniPoolError, match="too large"):
             U.quantize_mx8(U.BF16, 1, cols, P, P, P, stream=0)
+
+
+def test_balance_loss_of_the_most_tokens(U):
+    sh = shape(U, T=(1 << 31) - 63, k=1, E=1)
+    with pytest.raises(U.UniPoolError, match="2\\^31 - 64"):
+        U.seq_balance_loss(sh, 1, P, 0.1, P, P, P, P, None, None, Ws(1 << 60), stream=0)
