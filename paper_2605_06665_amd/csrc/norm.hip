@@ -338,7 +338,7 @@ hipError_t run_norm_bwd(NormBwdArgs a, float* d_weight, float* part, hipStream_t
     const bool wide = a.d % n == 0 && aligned16({a.h, a.weight, a.dy, a.dh, a.dx});
     int grid = 1;
     with_norm_form<TA>(a.d, wide, [&](auto nn, auto w, auto r) {
-        grid = std::min(kNormParts, w() == 1 ? cdiv(a.T, kBwdRows) : a.T);
+        grid = std::min(kNormParts, w() == 1 ? (a.T - 1) / kBwdRows + 1 : a.T);      // (T + 7 may pass 2^31)
         a.part = grid == 1 ? d_weight : part;
         rmsnorm_bwd_kernel<TA, nn(), w(), r()><<<grid, w() == 1 ? 64 * kBwdRows : 64 * w(), 0, st>>>(a);
     });

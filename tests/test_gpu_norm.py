@@ -241,3 +241,25 @@ def test_more_rows_than_a_launch_takes():
         y2, (q2, s2) = like(x[lo:hi]), mx8_of(n, d)
         U.rmsnorm(shape(n, d, "f32"), x[lo:hi].clone(), None, w, EPS, None, y2, q2, s2)
         assert torch.equal(y2, y[lo:hi]) and torch.equal(q2, q[lo:hi]) and torch.equal(s2, s[:, lo:hi])
+
+
+def test_backward_of_the_most_rows():
+    """Next to 2^31 rows of one value: the last ones as a call of their own, the weight's gradient against 64 bits."""
+    import torch
+    U, T, n = lib(), (1 << 31) - 5, 1000
+    sh = U.Shape(T=T, d_model=1, d_ff=64, E=1, k=1, L=1, dtype=U.F32, sigma=1.0, c=2.5, eps=1e-6, alpha_pool=0.01)
+    h, dy = torch.randn((T, 1), device="cuda"), torch.randn((T, 1), device="cuda")
+    w = torch.full((1,), 1.25, device="cuda")
+    dx, dw = torch.empty_like(h), torch.full((1,), float("nan"), device="cuda")
+    U.rmsnorm_bwd(sh, h, w, dy, None, 0.5, dx, dw, torch.empty(U.workspace_bytes(sh), dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    sh2, dx2 = shape(n, 1, "f32"), torch.empty((n, 1), device="cuda")
+    U.rmsnorm_bwd(sh2, h[-n:].clone(), w, dy[-n:].clone(), None, 0.5, dx2, torch.empty_like(dw), torch.empty(U.workspace_bytes(sh2), dtype=torch.uint8, device="cuda"))
+    assert torch.equal(dx[-n:], dx2)
+    want = terms = 0.0
+    for a, b in zip(h.split(1 << 28), dy.split(1 << 28)):
+        t = a.double()
+        t = b.double() * t / torch.sqrt(t * t + 0.5)
+        want, terms = want + float(t.sum()), terms + float(t.abs().sum())
+    # T / 4096 rows of a wavefront one after the other, then eight wavefronts and 512 workgroups
+    assert abs(float(dw) - want) <= (T / 4096.0 + 100) * 2.0 ** -24 * terms
