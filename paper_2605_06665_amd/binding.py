@@ -150,7 +150,9 @@ def _current_stream() -> int:
     if _STREAM_OF is None:
         import torch
         torch.cuda.current_device()          # sets the device up, if nothing has yet
-        _STREAM_OF, _DEVICE = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        # (in this order: another thread may come by between the two, and goes by the second)
+        _DEVICE = torch._C._cuda_getDevice
+        _STREAM_OF = torch._C._cuda_getCurrentRawStream
     return _STREAM_OF(_DEVICE())
 
 
