@@ -331,8 +331,8 @@ int unipool_seq_balance_loss(const unipool_shape* shape, int n_seq, const int32_
  * All of it in float, whose range also holds for the sum of h^2; y is made from the unrounded h.  y may leave as act, in 8 bits
  * (MX8, below), or both: the router reads the one, unipool_expert_ffn_fwd_mx8 the other.
  * in : x [T, d] act;  residual [T, d] act or NULL;  weight [d] act;  norm_eps >= 0;  d <= 16384.
- * out: h [T, d] act or NULL (may be x or residual itself);  y [T, d] act or NULL;  y_q [T, d] and y_scale in MX8, or both NULL
- *      (needs d to be a multiple of 32).  One of y and y_q must be given.
+ * out: h [T, d] act or NULL;  y [T, d] act or NULL;  y_q [T, d] and y_scale in MX8, or both NULL (needs d to be a multiple of 32).
+ *      One of y and y_q must be given.  h and y may each be x or residual itself, not both the same.
  */
 int unipool_rmsnorm(const unipool_shape* shape, const void* x, const void* residual, const void* weight, float norm_eps,
                     void* h, void* y, void* y_q, void* y_scale, void* stream);

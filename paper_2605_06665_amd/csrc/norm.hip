@@ -83,7 +83,8 @@ struct NormArgs {
     int row0;                 // first row of the launch
 };
 
-// W wavefronts share a row and hold it in R chunks of N values a lane.
+// W wavefronts share a row and hold it in R chunks of N values a lane.  h and y may lie in the place of x or of the residual: a lane has
+// read all of its chunks before it writes the first, and no lane reads another's.
 template <typename TA, int N, int W, int R>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rmsnorm_kernel(const NormArgs a) {
     typedef typename Pack<TA, N>::type P;

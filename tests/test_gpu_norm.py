@@ -263,3 +263,25 @@ def test_backward_of_the_most_rows():
         want, terms = want + float(t.sum()), terms + float(t.abs().sum())
     # T / 4096 rows of a wavefront one after the other, then eight wavefronts and 512 workgroups
     assert abs(float(dw) - want) <= (T / 4096.0 + 100) * 2.0 ** -24 * terms
+
+
+# rows of one, four and sixteen wavefronts, in chunks of 16 bytes and value by value
+@pytest.mark.parametrize("dtype,T,d", [("bf16", 9, 512), ("bf16", 7, 1536), ("bf16", 5, 4096), ("bf16", 3, 8192), ("bf16", 3, 16384), ("f32", 9, 252),
+                                       ("f32", 7, 1024), ("f32", 5, 2048), ("f32", 3, 16384), ("f32", 9, 31), ("f32", 5, 1023), ("f32", 3, 4099), ("f32", 2, 16381)])
+def test_outputs_in_the_place_of_inputs(dtype, T, d):
+    import torch
+    U, sh = lib(), shape(T, d, dtype)
+    x, r, w = (dev(rows(*n, dtype, i), dtype) for i, n in enumerate(((T, d), (T, d), (1, d))))
+    w = w[0].contiguous()
+    h, y = like(x), like(x)
+    U.rmsnorm(sh, x, r, w, EPS, h, y, None, None)
+    alone = like(x)
+    U.rmsnorm(sh, x, None, w, EPS, None, alone, None, None)
+    for y_at in (0, 1):
+        for h_at in (None, 1 - y_at):
+            a = [x.clone(), r.clone()]
+            U.rmsnorm(sh, *a, w, EPS, None if h_at is None else a[h_at], a[y_at], None, None)
+            assert torch.equal(a[y_at], y) and torch.equal(a[1 - y_at], h if h_at is not None else (x, r)[1 - y_at])
+    a = x.clone()
+    U.rmsnorm(sh, a, None, w, EPS, None, a, None, None)
+    assert torch.equal(a, alone)

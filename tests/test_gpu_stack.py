@@ -220,3 +220,23 @@ def test_stack_refuses_its_result_as_its_input():
     with pytest.raises(AssertionError, match="kept for the backward"):
         stack.forward(y, *args)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("d,L", [(128, 1), (2112, 1), (8256, 1), (2112, 3)])
+def test_serving_takes_its_own_result_with_any_number_of_layers(d, L):
+    """With one layer the last norm finds the residual where its result goes; rows of one, four and sixteen wavefronts."""
+    import torch
+    from paper_2605_06665_amd.pipeline import PoolServe
+    T, f, E, k = 20, 64, 4, 2
+    i = inputs(T, d, f, E, L, "bf16", 5)
+    sv = PoolServe(T, d, f, E, k, C, EPS, dev(np.concatenate([i["wg"], i["wu"]], axis=1), "bf16"), dev(i["wd"], "bf16"), norm_eps=NORM_EPS)
+    w = [dev(n, "bf16") for n in i["norms"]], [dev(n, "bf16") for n in i["wrs"]], i["sigmas"]
+    x = dev(i["x"], "bf16")
+    for n in (T, 3, 1):
+        want = x[:n].clone()
+        for _ in range(3):
+            want = sv.forward(want, *w).clone()
+        got = x[:n].clone()
+        for _ in range(3):
+            got = sv.forward(got, *w)
+        assert torch.equal(got, want)
