@@ -333,6 +333,16 @@ class PoolGroups:
             ps.step(xs[lo:hi], w_routers[lo:hi], sigmas[lo:hi], w_gate_up[g], w_down[g], grad_outs[lo:hi])
 
 
+def _fits(t, shape, like) -> bool:
+    """Whether t is what an entry point takes for granted: this shape, the type and device of `like`."""
+    return t.shape == shape and t.dtype == like.dtype and t.device == like.device
+
+
+def _shares(t, buffers) -> bool:
+    at = t.untyped_storage().data_ptr()
+    return any(at == b.untyped_storage().data_ptr() for b in buffers)
+
+
 class PoolStack:
     """The L layers of a PoolStep as the FFN sub-layers of a pre-norm transformer:
         h_0 = x;   y_l = norm(h_l);   h_{l+1} = h_l + layer_l(y_l);   result: y_L = norm(h_L).
@@ -349,9 +359,17 @@ class PoolStack:
         self.dx = torch.empty((T, d), **act)
         self.d_norm = torch.empty((L + 1, d), dtype=torch.float32, device=step.dev)
 
-    def forward(self, x, norm_weights, w_routers, sigmas, w_gate_up, w_down, fbar_in=None):
+    def _check(self, t, norm_weights, w_routers, sigmas):
         ps = self.step
-        assert x.data_ptr() != self.y[ps.L].data_ptr(), "x is kept for the backward pass; this call overwrites it with its result"
+        assert _fits(t, (ps.T, ps.d), self.dx), "x and grad_y are [T, d] of the step's type, on its device"
+        assert len(w_routers) == len(sigmas) == len(norm_weights) - 1 == ps.L
+        assert all(_fits(w, (ps.d,), self.dx) for w in norm_weights) and all(_fits(w, (ps.E, ps.d), self.dx) for w in w_routers)
+
+    def forward(self, x, norm_weights, w_routers, sigmas, w_gate_up, w_down, fbar_in=None):
+        """x is kept for the backward pass and may not be one of the stack's own buffers."""
+        ps = self.step
+        self._check(x, norm_weights, w_routers, sigmas)
+        assert not _shares(x, [*self.h[1:], *self.y, self.dx]), "x is kept for the backward pass; the stack writes over its own buffers"
         self.h[0] = x
         sh = ps.shape(1.0)
         ps._call(B.rmsnorm, sh, x, None, norm_weights[0], self.norm_eps, None, self.y[0], None, None)
@@ -364,6 +382,7 @@ class PoolStack:
     def backward(self, grad_y, norm_weights, w_routers, sigmas, w_gate_up, w_down):
         """Returns the gradient of x; the objective is <grad_y, y_L> plus the auxiliary losses."""
         ps, dx = self.step, self.dx
+        self._check(grad_y, norm_weights, w_routers, sigmas)
         sh = ps.shape(1.0)
         ps.begin_backward()
         # dx: the gradient of h_{l+1}, which is that of layer l's output and, along the residual, of h_l
@@ -415,9 +434,11 @@ class PoolServe:
 
     def layer(self, x, residual, h, norm_weight, w_router, sigma):
         """One sub-layer for x.shape[0] tokens: h = x + residual (residual None: h = x, and h may be None), returns the layer's output of
-        norm(h).  The output stays valid until the next call."""
+        norm(h).  The output stays valid until the next call, which may take it as its x or residual."""
         n = x.shape[0]
-        assert 1 <= n <= self.T and x.shape == (n, self.d) and x.dtype == torch.bfloat16
+        assert 1 <= n <= self.T and all(t is None or _fits(t, (n, self.d), self.out) for t in (x, residual, h))
+        assert _fits(norm_weight, (self.d,), self.out) and _fits(w_router, (self.E, self.d), self.out)
+        assert h is None or not _shares(h, (self.out, self.y)), "this call writes over h"
         sh, ws = self.shape(n, sigma), self.ws
         # (the first n rows of a buffer; scales of n rows are packed anew, since their layout goes by the number of rows)
         xs = self.x_q[1].view(-1)[:4 * n * -(-self.d // 128)]
@@ -433,9 +454,11 @@ class PoolServe:
 
     def forward(self, x, norm_weights, w_routers, sigmas):
         """All layers (as many as there are routers) and the final norm, as PoolStack.forward; x is left as it is.  The result stays
-        valid until the next call, which may take it as its x."""
+        valid until the next call, which may take it as its x; the output of layer() is not for that."""
         assert len(w_routers) == len(sigmas) == len(norm_weights) - 1 >= 1
-        n, h = x.shape[0], None
+        assert _fits(norm_weights[-1], (self.d,), self.out)
+        assert not _shares(x, (self.out, self.y, self.residual)), "x has to last for two layers; this call writes over it"
+        n = x.shape[0]
         for l, (w_router, sigma) in enumerate(zip(w_routers, sigmas)):
             if l == 0:
                 out = self.layer(x, None, None, norm_weights[0], w_router, sigma)

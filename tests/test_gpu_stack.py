@@ -240,3 +240,57 @@ def test_serving_takes_its_own_result_with_any_number_of_layers(d, L):
         for _ in range(3):
             got = sv.forward(got, *w)
         assert torch.equal(got, want)
+
+
+def test_serving_refuses_what_does_not_fit_argument_by_argument():
+    import torch
+    from paper_2605_06665_amd.pipeline import PoolServe
+    T, d, f, E, k, L = 20, 128, 64, 4, 2, 2
+    i = inputs(T, d, f, E, L, "bf16", 5)
+    sv = PoolServe(T, d, f, E, k, C, EPS, dev(np.concatenate([i["wg"], i["wu"]], axis=1), "bf16"), dev(i["wd"], "bf16"), norm_eps=NORM_EPS)
+    norms, wrs = [dev(n, "bf16") for n in i["norms"]], [dev(n, "bf16") for n in i["wrs"]]
+    x = dev(i["x"], "bf16")
+    r, h = torch.zeros_like(x), torch.empty_like(x)
+    good = dict(x=x, residual=r, h=h, norm_weight=norms[0], w_router=wrs[0], sigma=1.0)
+    for name, bad in (("x", x[:, :64].contiguous()), ("x", x.float()), ("x", x.cpu()), ("x", x[:0]), ("residual", r[:-1]), ("residual", r.float()), ("residual", r.cpu()),
+                      ("h", h[:-1]), ("h", h.float()), ("h", sv.out), ("h", sv.out[:T]), ("norm_weight", norms[0].float()), ("norm_weight", norms[0][:-1]),
+                      ("norm_weight", norms[0].cpu()), ("w_router", wrs[0].float()), ("w_router", wrs[0][:-1]), ("w_router", wrs[0].T.contiguous())):
+        with pytest.raises(AssertionError):
+            sv.layer(**{**good, name: bad})
+    out = sv.layer(**good)
+    with pytest.raises(AssertionError, match="two layers"):      # layer 0's output goes where this one lies, and layer 1 adds x to it
+        sv.forward(out, norms, wrs, i["sigmas"])
+    with pytest.raises(AssertionError):
+        sv.forward(x, norms[:L] + [norms[L].float()], wrs, i["sigmas"])
+    # what layer() does take: its output as the next one's x and residual
+    want = sv.layer(out.clone(), out.clone(), h, norms[1], wrs[1], 1.0).clone()
+    out = sv.layer(**good)
+    assert torch.equal(sv.layer(out, out, h, norms[1], wrs[1], 1.0), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_stack_refuses_what_does_not_fit_argument_by_argument(dtype):
+    import torch
+    from paper_2605_06665_amd.pipeline import PoolStack, PoolStep
+    from paper_2605_06665_amd import binding as B
+    T, d, f, E, k, L = 20, 64, 64, 4, 2, 2
+    i = inputs(T, d, f, E, L, dtype, 6)
+    stack = PoolStack(PoolStep(T, d, f, E, k, L, B.BF16 if dtype == "bf16" else B.F32, C, EPS, 0.01), NORM_EPS)
+    other = torch.float32 if dtype == "bf16" else torch.bfloat16
+    x, norms, wrs = dev(i["x"], dtype), [dev(n, dtype) for n in i["norms"]], [dev(n, dtype) for n in i["wrs"]]
+    pool = dev(np.concatenate([i["wg"], i["wu"]], axis=1), dtype), dev(i["wd"], dtype)
+    good = dict(x=x, norm_weights=norms, w_routers=wrs, sigmas=i["sigmas"], w_gate_up=pool[0], w_down=pool[1])
+    stack.forward(**good)
+    dx = stack.backward(x, *list(good.values())[1:])
+    for name, bad in (("x", x[:-1]), ("x", x.to(other)), ("x", x.cpu()), ("x", dx), ("x", stack.y[0]), ("x", stack.h[1]), ("norm_weights", norms[:L]),
+                      ("norm_weights", norms[:L] + [norms[L].to(other)]), ("norm_weights", [norms[0][:-1]] + norms[1:]), ("w_routers", wrs[:1]),
+                      ("w_routers", [wrs[0], wrs[1][:-1]]), ("w_routers", [wrs[0].to(other), wrs[1]]), ("sigmas", i["sigmas"][:1])):
+        with pytest.raises(AssertionError):
+            stack.forward(**{**good, name: bad})
+        if name != "x":
+            with pytest.raises(AssertionError):
+                stack.backward(**{("grad_y" if n == "x" else n): v for n, v in {**good, name: bad}.items()})
+    for bad in (x[:-1], x.to(other), x.cpu()):
+        with pytest.raises(AssertionError):
+            stack.backward(bad, *list(good.values())[1:])
+    torch.cuda.synchronize()
