@@ -454,15 +454,17 @@ class PoolServe:
 
     def forward(self, x, norm_weights, w_routers, sigmas):
         """All layers (as many as there are routers) and the final norm, as PoolStack.forward; x is left as it is.  The result stays
-        valid until the next call, which may take it as its x; the output of layer() is not for that."""
+        valid until the next call, which may take it, or rows of it, as its x; the output of layer() is not for that."""
         assert len(w_routers) == len(sigmas) == len(norm_weights) - 1 >= 1
         assert _fits(norm_weights[-1], (self.d,), self.out)
         assert not _shares(x, (self.out, self.y, self.residual)), "x has to last for two layers; this call writes over it"
         n = x.shape[0]
         for l, (w_router, sigma) in enumerate(zip(w_routers, sigmas)):
             if l == 0:
-                out = self.layer(x, None, None, norm_weights[0], w_router, sigma)
-                h = x
+                # with one layer the result goes out while x is read: other rows of the same buffer are copied first, by the norm
+                h = self.residual[:n] if len(w_routers) == 1 and _shares(x, (self.result,)) else None
+                out = self.layer(x, None, h, norm_weights[0], w_router, sigma)
+                h = x if h is None else h
             else:
                 out = self.layer(out, h, self.residual[:n], norm_weights[l], w_router, sigma)
                 h = self.residual[:n]

@@ -242,6 +242,21 @@ def test_serving_takes_its_own_result_with_any_number_of_layers(d, L):
         assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("L", [1, 2])
+def test_serving_takes_rows_of_its_own_result(L):
+    """Rows of the result as the next call's x: with one layer it is read while the result goes out over it."""
+    import torch
+    from paper_2605_06665_amd.pipeline import PoolServe
+    T, d, f, E, k = 900, 128, 64, 4, 2
+    i = inputs(T, d, f, E, L, "bf16", 5)
+    sv = PoolServe(T, d, f, E, k, C, EPS, dev(np.concatenate([i["wg"], i["wu"]], axis=1), "bf16"), dev(i["wd"], "bf16"), norm_eps=NORM_EPS)
+    w = [dev(n, "bf16") for n in i["norms"]], [dev(n, "bf16") for n in i["wrs"]], i["sigmas"]
+    x = dev(i["x"], "bf16")
+    for lo, hi in ((1, T), (T - 1, T), (300, 700), (0, 5)):
+        want = sv.forward(sv.forward(x, *w)[lo:hi].clone(), *w).clone()
+        assert torch.equal(sv.forward(sv.forward(x, *w)[lo:hi], *w), want)
+
+
 def test_serving_refuses_what_does_not_fit_argument_by_argument():
     import torch
     from paper_2605_06665_amd.pipeline import PoolServe
