@@ -562,6 +562,7 @@ template <bool GATE_UP, int BM, int BN, int NSX, int NSW> hipError_t run_tile(Mx
 //     29.2 / 31.3 / 35.4, 187 rows 49 / 44 / 50 / 46);
 //   256 weight rows beyond (192 experts of 1536 x 4096, 11 rows 716 / 729 / 653 / 691, 42 rows 759 / 760 / 712 / 734, 85 rows 1087 / 906 / 1007 / 789);
 //   192 rows where experts take several tiles of 128 (the 192 experts, 125 rows: 128 x 256 939, 192 x 256 869; 512 of 1024 x 704, 256 rows 582 / 567).
+// The pools named here are all that was measured; between their widths (few rows: 832 to 1536 in the shorter dimension) the lines are drawn, not found.
 enum Mx8Form { MX8_FEW, MX8_64x128, MX8_96x128, MX8_64x256, MX8_128x256, MX8_192x256 };
 Mx8Form mx8_form(const unipool_shape& s) {
     const double S = (double)s.T * s.k, used = s.E * -std::expm1(-S / s.E), r = S / used, most = r + 2.0 * std::sqrt(r);
@@ -782,7 +783,7 @@ hipError_t mx8_ffn_fwd(const unipool_shape& s, const void* x, const void* x_scal
     const Mx8Form form = mx8_form(s);
     const bool few = form == MX8_FEW;
     const long long S = (long long)s.T * s.k;
-    // A launch for the scales of gathered rows (6 us) where every one would be fetched for 32 tiles of columns or more, 3 million words and
+    // A launch for the scales of gathered rows (7 us) where every one would be fetched for 32 tiles of columns or more, 3 million words and
     // over in all (192 experts of 1536 x 4096, k = 2, 4001 tokens 734 -> 726 us, 8192 787 -> 773, 32768 1570 -> 1548; but 64 experts of
     // 768 x 2048, k = 8, 16384 tokens, 16 tiles of columns, 809 / 809, and 512 of 1024 x 704, k = 8, 16384 tokens 568 / 576).
     const int words = cdiv(s.d_model, kMxStep), tiles = cdiv(s.d_ff, 128);
