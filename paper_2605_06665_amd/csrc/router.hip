@@ -151,7 +151,9 @@ __global__ __launch_bounds__(256) void route_finalize_kernel(
 // ones past E zero.  A wavefront takes one round of 64 / GS tokens (dz_tokens_per_block): the rounds of a block of 64 tokens
 // waited for their loads one after the other, on a quarter of the wavefronts (all of unipool_route_bwd, us: 5999 tokens of 90
 // experts, d 832 39 -> 35; 16384 of 512, 1024 94 -> 84; 4000 of 400, 640 62 -> 45; 32768 of 192, 1536 123 -> 121).
-template <typename TA, int GS, int VPL>
+// ADD: d_logits is there.  One kernel that tests the pointer at every value made the calls without it slower too (this kernel alone, 16384
+// tokens of 512 experts 20 us, with the test 36; 32768 of 192 15, 27).
+template <typename TA, int GS, int VPL, bool ADD>
 __global__ __launch_bounds__(256) void route_bwd_dz_kernel(
     const float* __restrict__ logits, const int32_t* __restrict__ topk_idx,
     const float* __restrict__ dgate, const float* __restrict__ aux_coef, const float* __restrict__ d_logits,
@@ -233,7 +235,8 @@ __global__ __launch_bounds__(256) void route_bwd_dz_kernel(
                     const int e = sl + GS * i;
                     if (e < ldz) {
                         float v = e < E ? pr[i] * (ds[i] - dotp) : 0.f;
-                        if (d_logits != nullptr && e < E) v += d_logits[(size_t)t * E + e];
+                        if constexpr (ADD)
+                        if (e < E) v += d_logits[(size_t)t * E + e];
                         dz[(size_t)t * ldz + e] = from_f32<TA>(v);
                     }
                 }
@@ -259,7 +262,8 @@ __global__ __launch_bounds__(256) void route_bwd_dz_kernel(
                 const int e = sl + GS * i;
                 if (e < ldz) {
                     float v = (n > 0.f && e < E) ? dzh[i] * inv - z[i] * back : 0.f;
-                    if (d_logits != nullptr && e < E) v += d_logits[(size_t)t * E + e];
+                    if constexpr (ADD)
+                        if (e < E) v += d_logits[(size_t)t * E + e];
                     dz[(size_t)t * ldz + e] = from_f32<TA>(v);
                 }
             }
@@ -342,9 +346,12 @@ hipError_t launch_route_bwd_dz(const unipool_shape& s, const float* logits, cons
                                const float* dgate, const float* aux_coef, const float* d_logits, const float* d_sigma_in, void* dz,
                                float* dsigma_part, hipStream_t st) {
     const int tokens = dz_tokens_per_block(s), nblocks = cdiv(s.T, tokens);
-#define UNIPOOL_DZ(TA, GS, VPL)                                                                        \
-    route_bwd_dz_kernel<TA, GS, VPL><<<nblocks, 256, 0, st>>>(logits, topk_idx, dgate, aux_coef, d_logits, d_sigma_in, s.T, s.E, \
-                                                              s.k, s.sigma, s.c, s.eps, s.router, tokens, (TA*)dz, dz_stride(s), dsigma_part)
+    auto run = [&](auto kern, auto* z) {
+        kern<<<nblocks, 256, 0, st>>>(logits, topk_idx, dgate, aux_coef, d_logits, d_sigma_in, s.T, s.E, s.k, s.sigma, s.c, s.eps, s.router,
+                                      tokens, z, dz_stride(s), dsigma_part);
+    };
+#define UNIPOOL_DZ(TA, GS, VPL)                                                                                        \
+    d_logits != nullptr ? run(route_bwd_dz_kernel<TA, GS, VPL, true>, (TA*)dz) : run(route_bwd_dz_kernel<TA, GS, VPL, false>, (TA*)dz)
     if (s.dtype == UNIPOOL_BF16) {
         if (s.E <= 128) UNIPOOL_DZ(bf16, 16, 8);
         else if (s.E <= 256) UNIPOOL_DZ(bf16, 16, 16);

@@ -192,3 +192,32 @@ def test_dx_of_many_tokens_of_a_large_pool(T, accumulate):
     rows = torch.tensor([0, 127, 128, 255, 256, 65535, T - 257, T - 256, T - 255, T - 1], device="cuda")
     want = dz[rows] @ wr.double() + (0.5 if accumulate else 0.0)
     assert rel_err(host(dx[rows]), host(want)) <= TOL["bf16"]
+
+
+def test_calls_without_further_gradients_do_not_pay_for_them():
+    """65536 tokens of 512 experts, d 64: 3.3 times a conversion of the logits to bfloat16 (4 + 2 bytes a logit); 5.4 times with a kernel that looks for d_logits
+    at every value."""
+    import torch
+    import paper_2605_06665_amd as U
+    T, E, d, k = 65536, 512, 64, 2
+    sh = U.Shape(T=T, d_model=d, d_ff=64, E=E, k=k, L=1, dtype=U.BF16, sigma=1.0, c=2.5, eps=1e-6, alpha_pool=0.01)
+    x, w = torch.randn(T, d, device="cuda").bfloat16(), torch.randn(E, d, device="cuda").bfloat16()
+    z, dg = torch.randn(T, E, device="cuda"), torch.randn(T, k, device="cuda")
+    idx = torch.randint(0, E, (T, k), device="cuda").int()
+    ws = torch.empty(U.workspace_bytes(sh), dtype=torch.uint8, device="cuda")
+    dw, ds, dx, half = torch.empty(E, d, device="cuda"), torch.empty(1, device="cuda"), torch.empty_like(x), torch.empty(T, E, dtype=torch.bfloat16, device="cuda")
+
+    def best_time(f):
+        f()
+        times = []
+        for _ in range(6):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            for _ in range(20):
+                f()
+            b.record()
+            b.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+
+    assert best_time(lambda: U.route_bwd(sh, x, w, z, idx, dg, None, dw, ds, dx, False, ws)) <= 4.3 * best_time(lambda: half.copy_(z))
