@@ -79,7 +79,8 @@ def test_slots_of_rows_outside_the_offsets_are_not_looked_up(T, E, d, f, k):
 @pytest.mark.parametrize("form,first,T,E,d,f,k", [
     (0, False, 12, 6, 448, 256, 2), (64128, False, 180, 9, 448, 192, 2), (96128, False, 1500, 5, 384, 256, 4), (64256, False, 1344, 128, 384, 4224, 2),
     (128256, False, 3200, 64, 384, 4096, 2), (128256, True, 6720, 134, 832, 4096, 2),
-    (192256, False, 8192, 16, 384, 4096, 2), (192256, False, 8192, 12, 832, 2112, 3), (192256, True, 16384, 16, 384, 4160, 2), (192256, True, 9001, 10, 832, 4096, 3)])
+    (192256, False, 8192, 16, 384, 4096, 2), (192256, False, 8192, 12, 832, 2112, 3), (192256, True, 16384, 16, 384, 4160, 2), (192256, True, 9001, 10, 832, 4096, 3),
+    (192256, False, 38400, 512, 448, 64, 2)])
 def test_every_row_of_wide_tiles_is_the_one_looked_up(form, first, T, E, d, f, k):
     """All rows against rows in group order, bit for bit; rows spread over all the tiles of some experts against 64 bits."""
     import torch
