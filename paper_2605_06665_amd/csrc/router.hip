@@ -236,7 +236,7 @@ __global__ __launch_bounds__(256) void route_bwd_dz_kernel(
                     if (e < ldz) {
                         float v = e < E ? pr[i] * (ds[i] - dotp) : 0.f;
                         if constexpr (ADD)
-                        if (e < E) v += d_logits[(size_t)t * E + e];
+                            if (e < E) v += d_logits[(size_t)t * E + e];
                         dz[(size_t)t * ldz + e] = from_f32<TA>(v);
                     }
                 }

@@ -359,16 +359,17 @@ class PoolStack:
         self.dx = torch.empty((T, d), **act)
         self.d_norm = torch.empty((L + 1, d), dtype=torch.float32, device=step.dev)
 
-    def _check(self, t, norm_weights, w_routers, sigmas):
+    def _check(self, t, norm_weights, w_routers, sigmas, w_gate_up, w_down):
         ps = self.step
         assert _fits(t, (ps.T, ps.d), self.dx), "x and grad_y are [T, d] of the step's type, on its device"
         assert len(w_routers) == len(sigmas) == len(norm_weights) - 1 == ps.L
         assert all(_fits(w, (ps.d,), self.dx) for w in norm_weights) and all(_fits(w, (ps.E, ps.d), self.dx) for w in w_routers)
+        assert _fits(w_gate_up, (ps.E, 2 * ps.f, ps.d), self.dx) and _fits(w_down, (ps.E, ps.d, ps.f), self.dx)
 
     def forward(self, x, norm_weights, w_routers, sigmas, w_gate_up, w_down, fbar_in=None):
         """x is kept for the backward pass and may not be one of the stack's own buffers."""
         ps = self.step
-        self._check(x, norm_weights, w_routers, sigmas)
+        self._check(x, norm_weights, w_routers, sigmas, w_gate_up, w_down)
         assert not _shares(x, [*self.h[1:], *self.y, self.dx]), "x is kept for the backward pass; the stack writes over its own buffers"
         self.h[0] = x
         sh = ps.shape(1.0)
@@ -382,7 +383,7 @@ class PoolStack:
     def backward(self, grad_y, norm_weights, w_routers, sigmas, w_gate_up, w_down):
         """Returns the gradient of x; the objective is <grad_y, y_L> plus the auxiliary losses."""
         ps, dx = self.step, self.dx
-        self._check(grad_y, norm_weights, w_routers, sigmas)
+        self._check(grad_y, norm_weights, w_routers, sigmas, w_gate_up, w_down)
         sh = ps.shape(1.0)
         ps.begin_backward()
         # dx: the gradient of h_{l+1}, which is that of layer l's output and, along the residual, of h_l
@@ -404,6 +405,7 @@ class PoolServe:
         assert router in ("norm", "softmax")
         assert w_gate_up.shape == (E, 2 * d_ff, d_model) and w_down.shape == (E, d_model, d_ff)
         assert w_gate_up.dtype == w_down.dtype == torch.bfloat16
+        assert w_gate_up.is_cuda and w_down.device == w_gate_up.device
         self.T, self.d, self.f, self.E, self.k = T, d_model, d_ff, E, k
         self.c, self.eps, self.norm_eps = c, eps, float(norm_eps)
         self.router = B.ROUTER_SOFTMAX if router == "softmax" else B.ROUTER_NORM

@@ -309,3 +309,24 @@ def test_stack_refuses_what_does_not_fit_argument_by_argument(dtype):
         with pytest.raises(AssertionError):
             stack.backward(bad, *list(good.values())[1:])
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_stack_refuses_a_pool_that_does_not_fit(dtype):
+    import torch
+    from paper_2605_06665_amd.pipeline import PoolStack, PoolStep
+    from paper_2605_06665_amd import binding as B
+    T, d, f, E, k, L = 20, 64, 128, 4, 2, 1
+    i = inputs(T, d, f, E, L, dtype, 6)
+    stack = PoolStack(PoolStep(T, d, f, E, k, L, B.BF16 if dtype == "bf16" else B.F32, C, EPS, 0.01), NORM_EPS)
+    other = torch.float32 if dtype == "bf16" else torch.bfloat16
+    x, norms, wrs = dev(i["x"], dtype), [dev(n, dtype) for n in i["norms"]], [dev(n, dtype) for n in i["wrs"]]
+    gu, down = dev(np.concatenate([i["wg"], i["wu"]], axis=1), dtype), dev(i["wd"], dtype)
+    stack.forward(x, norms, wrs, i["sigmas"], gu, down)
+    for pool in ((gu[:-1], down), (gu[:, :f].contiguous(), down), (gu.to(other), down), (gu.cpu(), down), (gu, down[:-1]), (gu, down.to(other)),
+                 (gu, down.cpu()), (gu, down.transpose(1, 2).contiguous()), (down, gu)):
+        for call in (stack.forward, stack.backward):
+            with pytest.raises(AssertionError):
+                call(x, norms, wrs, i["sigmas"], *pool)
+    stack.backward(x, norms, wrs, i["sigmas"], gu, down)
+    torch.cuda.synchronize()

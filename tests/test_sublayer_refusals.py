@@ -142,3 +142,13 @@ def test_balance_loss_of_the_most_tokens(U):
     sh = shape(U, T=(1 << 31) - 63, k=1, E=1)
     with pytest.raises(U.UniPoolError, match="2\\^31 - 64"):
         U.seq_balance_loss(sh, 1, P, 0.1, P, P, P, P, None, None, Ws(1 << 60), stream=0)
+
+
+def test_serving_refuses_weights_that_are_not_on_the_device(U):
+    import torch
+    from paper_2605_06665_amd.pipeline import PoolServe
+    T, d, f, E, k = 8, 64, 64, 4, 2
+    w = torch.zeros(E, 2 * f, d, dtype=torch.bfloat16), torch.zeros(E, d, f, dtype=torch.bfloat16)
+    for bad in (w, (w[0].float(), w[1]), (w[0], w[1][:-1])):
+        with pytest.raises(AssertionError):
+            PoolServe(T, d, f, E, k, 2.5, 1e-6, *bad)
