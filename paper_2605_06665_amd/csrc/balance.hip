@@ -8,7 +8,7 @@
 // then gives loss and gradient.  The score is linear in sigma: d loss / d sigma = loss / sigma (softmax: 0).
 //
 // Bound by memory and by what a token costs in instructions and latency: 4 bytes in and 4 out per logit.  16384 tokens of 512
-// experts, k = 8, 37 sequences, softmax: counts 4.9 us, loss and gradient 19.1 us (67 MB, 3.5 TB/s;
+// experts, k = 8, 37 sequences, softmax: counts 4.9 us, loss and gradient 19 to 20 us (67 MB, 3.4 TB/s;
 // without the gradient's stores 4.8 us less, without the sum over the workgroups 2 less, without the search for the sequence 1 less).
 // A sequence is counted in parts by the average length, as lengths are known on the device only: one that is much longer than the others
 // keeps few workgroups busy while the rest of the card waits (131072 tokens of 512 experts, k = 8: 33 even sequences 125 us, 32 of
